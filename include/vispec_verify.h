@@ -21,6 +21,11 @@
  *                             image embeddings (Section 4.1, Fig. 3)
  *   vs_tree_kv_commit         keeps the accepted path's K/V rows, in order, behind the
  *                             prefix of the pre-allocated cache (Section 3.1, Appendix A)
+ *   vs_rope_apply             rotary positions of one to four axes (time, height, width of image and
+ *                             video embeddings) on rows of heads, and the rotation back
+ *   vs_kv_append              what stands in front of the attention in every layer: new queries and keys
+ *                             rotated by their positions, new keys and values into the caches behind the
+ *                             prefixes (prompts, draft trees, single tokens)
  *
  * Conventions
  *   - C ABI, no exceptions cross it. Every function returns an int32 vs_error
@@ -72,8 +77,9 @@ typedef enum vs_status {
     VS_STATUS_BAD_PREFIX = 3, /* prefix_len < 0, > max_prefix_len, or prefix_len + T beyond the cache */
     VS_STATUS_BAD_BLOCK = 4,  /* a block-table entry in use lies outside [0, num_blocks) */
     VS_STATUS_BAD_PATH = 5,   /* accepted_len outside [0, T) or path not 0 followed by increasing node ids */
-    VS_STATUS_BAD_CANDIDATE = 6 /* draft tree: cand_parent outside [-1, index), or a selected candidate whose
+    VS_STATUS_BAD_CANDIDATE = 6, /* draft tree: cand_parent outside [-1, index), or a selected candidate whose
                                    parent was not selected (a child scoring above its parent) */
+    VS_STATUS_BAD_ROWS = 7      /* row_start: a sequence's rows end before they start, lie outside the call's or are more than T */
 } vs_status;
 
 typedef enum vs_dtype { VS_BF16 = 0, VS_F32 = 1 } vs_dtype;
@@ -416,6 +422,86 @@ typedef struct vs_kv_desc {
 int32_t vs_tree_kv_commit(const vs_kv_desc* desc, void* k_cache, void* v_cache, const int32_t* prefix_len,
                           const int32_t* path, const int32_t* accepted_len, int32_t* new_prefix_len,
                           int32_t* status, void* stream);
+
+/*
+ * Rotary positions (host struct, read during the call). The first rot_dim channels of a head are rot_dim / 2 pairs;
+ * pair i of a row turns by the angle (position of the row on the pair's axis) * inv_freq[i]:
+ *   (x, y) -> (x cos a - y sin a, y cos a + x sin a)
+ * and the other channels stay as they are. Angles are taken in 64 bits before their whole turns are dropped, so that positions
+ * far out lose nothing (an error below 5e-10 radians at positions up to 2^20, 5e-7 over all of int32), the rest is fp32,
+ * rounded once to the storage type. inv_freq is the caller's, so that any scaling of the frequencies is, too; the usual one is
+ * inv_freq[i] = theta^(-2 i / rot_dim).
+ *   Axes: images and video have positions in time, height and width, text the same position on all of them. axis_pairs[x] is
+ *   the number of pairs of axis x. VS_AXES_BLOCKS: the first axis_pairs[0] pairs belong to axis 0, the next to axis 1 and so
+ *   on. VS_AXES_CYCLIC: pair i belongs to axis i % num_axes while that axis (not the first) has pairs left, i / num_axes <
+ *   axis_pairs[i % num_axes], else to axis 0.
+ */
+typedef enum vs_rope_pairing { VS_PAIR_HALVES = 0, VS_PAIR_ADJACENT = 1 } vs_rope_pairing;
+typedef enum vs_axis_order { VS_AXES_BLOCKS = 0, VS_AXES_CYCLIC = 1 } vs_axis_order;
+
+typedef struct vs_rope_desc {
+    int32_t rot_dim;       /* 0 .. d; a multiple of 16 bytes' channels, with VS_PAIR_HALVES half of it is */
+    int32_t pairing;       /* vs_rope_pairing: channels i and i + rot_dim / 2, or 2 i and 2 i + 1 */
+    int32_t num_axes;      /* 1 .. 4 */
+    int32_t axis_order;    /* vs_axis_order */
+    int32_t axis_pairs[4]; /* their sum is rot_dim / 2; num_axes = 1: not read */
+    int32_t inverse;       /* nonzero: turns by the negative angle. That undoes the rotation, and is its gradient */
+    int64_t stride_axis;   /* elements from one axis's positions to the next's (0: one position for all axes) */
+    const double* inv_freq; /* device [rot_dim / 2], radians per position (may be NULL where rot_dim is 0) */
+} vs_rope_desc;
+
+/*
+ * Rotates `rows` rows of H heads of d channels.
+ *   x          in; head h of row r begins at r * x_stride_row + h * x_stride_head elements (the heads of a fused projection, for example)
+ *   positions  int32 in; row r's position on axis x is positions[x * stride_axis + r]
+ *   out        out, likewise with its strides; may be x itself with the same strides, and overlaps it in no other way
+ * With inverse set and the output's gradient as x, out is the gradient with respect to the rotation's input.
+ * rows < 2^31; d up to 256; d, the strides and the pointers are multiples of 16 bytes.
+ */
+int32_t vs_rope_apply(const vs_rope_desc* rope, const void* x, int64_t x_stride_row, int64_t x_stride_head,
+                      const int32_t* positions, int64_t rows, int32_t H, int32_t d, int32_t dtype, void* out,
+                      int64_t out_stride_row, int64_t out_stride_head, void* stream);
+
+/*
+ * New rows of one layer (host struct, read during the call). The caches' layout is vs_attn_desc's.
+ */
+typedef struct vs_append_desc {
+    int32_t B;      /* sequences */
+    int32_t T;      /* new rows per sequence; with row_start: the most of any sequence. 1 or more, no upper limit of its own */
+    int32_t Hq;     /* query heads; 0: keys and values only */
+    int32_t Hkv;
+    int32_t d;      /* up to 256 */
+    int32_t dtype;  /* vs_dtype of all tensors */
+    int64_t rows;   /* rows of q, k, v and q_out: B * T, with row_start the size of the buffers */
+    int64_t q_stride, k_stride, v_stride, q_out_stride; /* elements from row to row; a row's heads are dense */
+    int32_t paged, block_size, max_blocks, num_blocks;
+    int64_t capacity, stride_seq, stride_block, stride_head, stride_tok;
+    const int32_t* block_table; /* paged: device [B, max_blocks] */
+} vs_append_desc;
+
+/*
+ * Appends new tokens to the caches of one layer, their positions applied on the way.
+ * Sequence b's row i lies at row b * T + i of q, k and v, or with row_start (packed sequences of any lengths, 0 among them) at row
+ * row_start[b] + i, i < row_start[b + 1] - row_start[b]. Its keys and values go to logical slot prefix_len[b] + i of the
+ * sequence's cache: where vs_tree_verify_attention looks for a tree's nodes, and where the next tokens of a prompt belong.
+ *   q            in, rows of Hq heads (NULL with Hq = 0)
+ *   k, v         in, rows of Hkv heads (the three may be parts of one fused projection)
+ *   positions    int32 in, optional: row r's position on axis x is positions[x * stride_axis + r]. NULL: prefix_len[b] +
+ *                pos_offset[b] + (depth[b * T + i], or i without depth), the same on all axes
+ *   depth        [B,T] int32 in, optional, vs_tree_mask_build's (not together with row_start)
+ *   pos_offset   [B] int32 in, optional: what a sequence's positions are ahead of its slots (images take more slots than positions)
+ *   prefix_len   [B] int32 in
+ *   row_start    [B+1] int32 in, optional, ascending. Where it descends the sequence is reported, and the rows of all are unspecified
+ *   q_out        out, the rotated queries, rows of Hq heads; may be q itself with q's stride, and overlaps the inputs in no other way
+ *   k_cache, v_cache  out
+ *   status       [B] int32 out, optional: VS_STATUS_BAD_PREFIX, VS_STATUS_BAD_BLOCK, VS_STATUS_BAD_ROWS
+ * Rows of q_out behind the last sequence's and all other slots keep what they hold. Two new tokens never share a slot: no two sequences of a call
+ * have the same block where new rows go. prefix_len stays; the caller adds the rows to it, or vs_tree_kv_commit the accepted ones.
+ * rope->inverse has to be 0. d, strides and pointers are multiples of 16 bytes; rows and B * T stay below 2^31.
+ */
+int32_t vs_kv_append(const vs_append_desc* desc, const vs_rope_desc* rope, const void* q, const void* k, const void* v,
+                     const int32_t* positions, const int32_t* depth, const int32_t* pos_offset, const int32_t* prefix_len,
+                     const int32_t* row_start, void* q_out, void* k_cache, void* v_cache, int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

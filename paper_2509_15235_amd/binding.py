@@ -15,6 +15,8 @@ _LIB_PATH = os.environ.get("VISPEC_VERIFY_LIB") or os.path.join(_HERE, "libvispe
 VS_BF16, VS_F32 = 0, 1
 VS_IMPL_AUTO, VS_IMPL_GENERIC, VS_IMPL_MFMA = 0, 1, 2
 VS_SCHED_AUTO, VS_SCHED_LOOP, VS_SCHED_PIPELINED, VS_SCHED_RESIDENT, VS_SCHED_BALANCED = 0, 1, 2, 3, 4
+VS_PAIR_HALVES, VS_PAIR_ADJACENT = 0, 1
+VS_AXES_BLOCKS, VS_AXES_CYCLIC = 0, 1
 
 EXPORTED_SYMBOLS = [
     "vs_version", "vs_strerror", "vs_status_string", "vs_tree_validate_host", "vs_tree_mask_build",
@@ -22,6 +24,7 @@ EXPORTED_SYMBOLS = [
     "vs_accept_workspace_bytes", "vs_tree_accept", "vs_tree_accept_noalloc", "vs_accept_sample_workspace_bytes", "vs_tree_accept_sample",
     "vs_draft_expand_workspace_bytes", "vs_draft_expand", "vs_draft_tree_build", "vs_tree_kv_commit",
     "vs_compress_attention_workspace_bytes", "vs_compress_attention",
+    "vs_rope_apply", "vs_kv_append",
 ]
 # measurement helpers declared in include/vispec_peaks.h
 PEAK_SYMBOLS = ["vs_peak_hbm_read", "vs_peak_hbm_copy", "vs_peak_mfma_bf16", "vs_peak_mfma_flops"]
@@ -52,6 +55,25 @@ class KVDesc(ctypes.Structure):
         ("dtype", ctypes.c_int32), ("num_layers", ctypes.c_int32), ("stride_layer", ctypes.c_int64),
         ("paged", ctypes.c_int32), ("block_size", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
         ("num_blocks", ctypes.c_int32), ("capacity", ctypes.c_int64), ("stride_seq", ctypes.c_int64),
+        ("stride_block", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_tok", ctypes.c_int64),
+        ("block_table", ctypes.c_void_p),
+    ]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [
+        ("rot_dim", ctypes.c_int32), ("pairing", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("axis_order", ctypes.c_int32),
+        ("axis_pairs", ctypes.c_int32 * 4), ("inverse", ctypes.c_int32), ("stride_axis", ctypes.c_int64),
+        ("inv_freq", ctypes.c_void_p),
+    ]
+
+
+class AppendDesc(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("T", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("rows", ctypes.c_int64), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64), ("paged", ctypes.c_int32), ("block_size", ctypes.c_int32),
+        ("max_blocks", ctypes.c_int32), ("num_blocks", ctypes.c_int32), ("capacity", ctypes.c_int64), ("stride_seq", ctypes.c_int64),
         ("stride_block", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_tok", ctypes.c_int64),
         ("block_table", ctypes.c_void_p),
     ]
@@ -121,6 +143,10 @@ def lib():
         L.vs_draft_tree_build.restype = i32
         L.vs_tree_kv_commit.argtypes = [ctypes.POINTER(KVDesc), vp, vp, vp, vp, vp, vp, vp, vp]
         L.vs_tree_kv_commit.restype = i32
+        L.vs_rope_apply.argtypes = [ctypes.POINTER(RopeDesc), vp, i64, i64, vp, i64, i32, i32, i32, vp, i64, i64, vp]
+        L.vs_rope_apply.restype = i32
+        L.vs_kv_append.argtypes = [ctypes.POINTER(AppendDesc), ctypes.POINTER(RopeDesc)] + [vp] * 13
+        L.vs_kv_append.restype = i32
         L.vs_peak_hbm_read.argtypes = [vp, sz, vp, i32, vp]
         L.vs_peak_hbm_read.restype = i32
         L.vs_peak_hbm_copy.argtypes = [vp, vp, sz, i32, vp]
@@ -168,16 +194,18 @@ def _scalar(code, x):
 # pointers as _ptr takes them, the trailing optional ones None / 0 by default
 _NATIVE = ("vs_tree_mask_build", "vs_tree_verify_attention", "vs_compress_attention", "vs_tree_accept", "vs_tree_accept_noalloc",
            "vs_tree_accept_sample", "vs_draft_expand", "vs_draft_tree_build", "vs_tree_kv_commit")
+# the same for calls that take descriptors of other kinds, or more than one
+_NATIVE_MORE = ("vs_rope_apply", "vs_kv_append")
 
 
 def _load_native():
     loaded = lib()
-    _native.bind({name: ctypes.cast(getattr(loaded, name), ctypes.c_void_p).value for name in _NATIVE})
+    _native.bind({name: ctypes.cast(getattr(loaded, name), ctypes.c_void_p).value for name in _NATIVE + _NATIVE_MORE})
 
 
 def _missing(name):
     def call(*args, **kwargs):
-        raise FileNotFoundError(f"{os.path.join(_HERE, '_native.so')} is missing: build it with `python -m paper_2509_15235_amd.build`")
+        raise FileNotFoundError(f"{os.path.join(_HERE, '_native.so')} is missing or out of date: build it with `python -m paper_2509_15235_amd.build`")
     call.__name__ = name
     return call
 
@@ -187,10 +215,13 @@ try:
 except ImportError:
     if os.path.exists(os.path.join(_HERE, "_native.so")):
         raise
-    globals().update({name: _missing(name) for name in _NATIVE})
+    globals().update({name: _missing(name) for name in _NATIVE + _NATIVE_MORE})
 else:
-    _native.setup(_load_native, _ptr, _scalar, ctypes.byref, ctypes.ArgumentError, AttnDesc, KVDesc)
-    globals().update({name: getattr(_native, name) for name in _NATIVE})
+    try:
+        _native.setup(_load_native, _ptr, _scalar, ctypes.byref, ctypes.ArgumentError, AttnDesc, KVDesc, RopeDesc, AppendDesc)
+        globals().update({name: getattr(_native, name) for name in _NATIVE + _NATIVE_MORE})
+    except (TypeError, AttributeError):  # built from other sources than these: the package can still be imported to build it
+        globals().update({name: _missing(name) for name in _NATIVE + _NATIVE_MORE})
 
 
 def vs_version() -> int:

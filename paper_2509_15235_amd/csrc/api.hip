@@ -13,8 +13,6 @@ using namespace vs;
 
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-inline bool is_pow2(int32_t x) { return x > 0 && (x & (x - 1)) == 0; }
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 } // namespace
 
@@ -605,6 +603,7 @@ const char* vs_status_string(int32_t code) {
     case VS_STATUS_BAD_PREFIX: return "prefix_len outside the cache or the host bound";
     case VS_STATUS_BAD_BLOCK: return "a block-table entry is outside the pool";
     case VS_STATUS_BAD_PATH: return "accepted path is not the root followed by increasing node ids";
+    case VS_STATUS_BAD_ROWS: return "row_start is not ascending, leaves the call's rows or gives a sequence more than T";
     case VS_STATUS_BAD_CANDIDATE: return "a candidate's parent is not an earlier candidate, or a child outscores its parent";
     default: return "unknown status";
     }

@@ -179,6 +179,58 @@ struct CommitParams {
     int64_t stride_layer_bytes, stride_seq_bytes, stride_block_bytes, stride_head_bytes, stride_tok_bytes;
 };
 
+constexpr int kMaxRopePairs = 128; // of a head of 256 channels
+
+// A rotation, for the kernels.
+struct RopeParams {
+    const double* inv_freq;      // [pairs]
+    int64_t stride_axis;
+    int32_t pairs;               // rotated channels / 2
+    int32_t num_axes, cyclic, inverse;
+    int32_t axis_pairs[4];
+    int32_t turning;             // items of a head that turn (rope_device.h)
+    int32_t chunks;              // ... and all of them
+    FastDiv by_chunks;
+};
+
+struct RopeApplyParams {
+    const void* x;
+    void* out;
+    const int32_t* positions;
+    int64_t rows;
+    int64_t x_row, x_head, out_row, out_head; // strides in bytes
+    int32_t H;
+    int32_t rows_per_wg, heads_per_wg;
+    FastDiv by_heads;            // heads_per_wg
+    RopeParams rope;
+};
+
+struct AppendParams {
+    const void* q;
+    const void* k;
+    const void* v;
+    const int32_t* positions;    // may be null
+    const int32_t* depth;        // may be null
+    const int32_t* pos_offset;   // may be null
+    const int32_t* prefix_len;
+    const int32_t* row_start;    // may be null: B * T rows
+    void* q_out;
+    void* k_cache;
+    void* v_cache;
+    int32_t* status;             // may be null
+    const int32_t* block_table;  // paged only
+    int64_t rows;
+    int64_t q_row, k_row, v_row, q_out_row; // strides in bytes
+    int32_t B, T, Hq, Hkv;
+    int32_t row_bytes;           // of a head
+    int32_t rows_per_wg, heads_per_wg;
+    int32_t paged, block_size, block_shift, max_blocks, num_blocks;
+    FastDiv by_T, by_heads;      // T, heads_per_wg
+    int64_t capacity;
+    int64_t stride_seq, stride_block, stride_head, stride_tok; // bytes
+    RopeParams rope;
+};
+
 // Shared tree check: returns a vs_status for lane-parallel use is in the kernels; this is
 // the scalar form used on the host.
 inline int32_t validate_tree_host(const int32_t* parent, int32_t T) {
@@ -193,6 +245,8 @@ extern "C" void vs_internal_set_merge_wait(uint32_t ticks);
 // Whether a call with this descriptor loads K and V as data that is read once (1 or 0; or a vs_error): for tests, the plan does not say.
 extern "C" int32_t vs_internal_reads_once(const vs_attn_desc* desc, int32_t tree);
 
+inline bool is_pow2(int32_t x) { return x > 0 && (x & (x - 1)) == 0; }
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 int32_t check_device(); // VS_OK when the current device is a gfx950, else VS_ERR_NO_DEVICE (api.hip)
 
 hipError_t launch_tree_mask(const int32_t* parent, int32_t B, int32_t T, uint64_t* mask,
@@ -214,5 +268,7 @@ hipError_t launch_accept_sample(SampleParams p, void* workspace, hipStream_t s);
 hipError_t launch_draft_expand(const DraftExpandParams& p, hipStream_t s);
 hipError_t launch_draft_tree_build(const DraftBuildParams& p, hipStream_t s);
 hipError_t launch_kv_commit(const CommitParams& p, hipStream_t s);
+hipError_t launch_rope(const RopeApplyParams& p, int dtype, bool halves, hipStream_t s);
+hipError_t launch_kv_append(const AppendParams& p, int dtype, bool halves, hipStream_t s);
 
 } // namespace vs
