@@ -26,6 +26,8 @@
  *   vs_kv_append              what stands in front of the attention in every layer: new queries and keys
  *                             rotated by their positions, new keys and values into the caches behind the
  *                             prefixes (prompts, draft trees, single tokens)
+ *   vs_shared_prefix_attention  vs_tree_verify_attention for a batch whose sequences begin with the same tokens,
+ *                             stored once (several questions about one image, one system prompt)
  *
  * Conventions
  *   - C ABI, no exceptions cross it. Every function returns an int32 vs_error
@@ -221,6 +223,44 @@ int32_t vs_tree_verify_attention(const vs_attn_desc* desc, const void* q, const 
                                  const int32_t* tree_parent, const uint64_t* tree_mask, void* out,
                                  int32_t* status, void* workspace, size_t workspace_bytes,
                                  void* stream);
+
+/*
+ * The keys that all sequences of a batch begin with, stored once (host struct, read during the call). Element offset of (KV head kv,
+ * token t, channel c):
+ *   contiguous (paged = 0):  kv*stride_head + t*stride_tok + c
+ *   paged      (paged = 1):  blk*stride_block + kv*stride_head + (t % block_size)*stride_tok + c  with  blk = block_table[t / block_size]
+ */
+typedef struct vs_prefix_desc {
+    int32_t max_len;        /* host-side upper bound on *shared_len, >= 1; sizes the launch */
+    int32_t paged, block_size, max_blocks, num_blocks; /* as in vs_attn_desc */
+    int64_t capacity;       /* contiguous: token slots (for the bounds check) */
+    int64_t stride_block;   /* paged */
+    int64_t stride_head, stride_tok;
+    const int32_t* block_table; /* paged: device [max_blocks] */
+} vs_prefix_desc;
+
+size_t vs_shared_prefix_workspace_bytes(const vs_attn_desc* desc, const vs_prefix_desc* prefix); /* 0 on invalid descriptors */
+
+/*
+ * Tree-masked attention of a batch behind a shared prefix: what vs_tree_verify_attention computes for sequences whose context is the
+ * *shared_len tokens that all of them have followed by prefix_len[b] tokens of their own. The shared keys and values are read once for all
+ * sequences instead of once for each, and multiplied with all sequences' queries as one matrix. T = 1 is a decoded token.
+ * The descriptor and the arguments describe the sequences' own caches as for vs_tree_verify_attention, with these differences:
+ *   - prefix_len[b] (>= 0, at most max_prefix_len) counts the sequence's own tokens only, and its cache holds only those, from logical
+ *     slot 0 on, and the tree's nodes behind them. (A paged program with one table row per sequence that names the shared blocks too
+ *     passes the address of the rows' first entry of their own, with max_blocks the row length as before; a shared prefix that
+ *     ends inside a block has its last tokens copied into the sequences' own blocks.) vs_kv_append and vs_tree_kv_commit work on such caches as they are.
+ *   - the knobs (impl, num_splits, rows_per_wave, waves_per_group, schedule) have to be 0
+ *   k_shared, v_shared  in, layout per prefix (may be the same pools as k_cache and v_cache)
+ *   shared_len   [1] int32  in, 0 .. max_len; anything else is VS_STATUS_BAD_PREFIX for all sequences, a bad block id
+ *                VS_STATUS_BAD_BLOCK for all
+ *   workspace    at least vs_shared_prefix_workspace_bytes(desc, prefix) bytes, 256-byte aligned
+ * The parts of a row's softmax are joined in fp32 before the one rounding to the storage type. B * T * (Hq / Hkv) is at most 1048576.
+ */
+int32_t vs_shared_prefix_attention(const vs_attn_desc* desc, const vs_prefix_desc* prefix, const void* q, const void* k_shared,
+                                   const void* v_shared, const int32_t* shared_len, const void* k_cache, const void* v_cache,
+                                   const int32_t* prefix_len, const int32_t* tree_parent, const uint64_t* tree_mask, void* out,
+                                   int32_t* status, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Compression attention of the vision adaptor (Section 4.1, Fig. 3: the adaptor owns a small,

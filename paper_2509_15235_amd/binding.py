@@ -24,7 +24,7 @@ EXPORTED_SYMBOLS = [
     "vs_accept_workspace_bytes", "vs_tree_accept", "vs_tree_accept_noalloc", "vs_accept_sample_workspace_bytes", "vs_tree_accept_sample",
     "vs_draft_expand_workspace_bytes", "vs_draft_expand", "vs_draft_tree_build", "vs_tree_kv_commit",
     "vs_compress_attention_workspace_bytes", "vs_compress_attention",
-    "vs_rope_apply", "vs_kv_append",
+    "vs_rope_apply", "vs_kv_append", "vs_shared_prefix_workspace_bytes", "vs_shared_prefix_attention",
 ]
 # measurement helpers declared in include/vispec_peaks.h
 PEAK_SYMBOLS = ["vs_peak_hbm_read", "vs_peak_hbm_copy", "vs_peak_mfma_bf16", "vs_peak_mfma_flops"]
@@ -76,6 +76,14 @@ class AppendDesc(ctypes.Structure):
         ("max_blocks", ctypes.c_int32), ("num_blocks", ctypes.c_int32), ("capacity", ctypes.c_int64), ("stride_seq", ctypes.c_int64),
         ("stride_block", ctypes.c_int64), ("stride_head", ctypes.c_int64), ("stride_tok", ctypes.c_int64),
         ("block_table", ctypes.c_void_p),
+    ]
+
+
+class PrefixDesc(ctypes.Structure):
+    _fields_ = [
+        ("max_len", ctypes.c_int32), ("paged", ctypes.c_int32), ("block_size", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+        ("num_blocks", ctypes.c_int32), ("capacity", ctypes.c_int64), ("stride_block", ctypes.c_int64), ("stride_head", ctypes.c_int64),
+        ("stride_tok", ctypes.c_int64), ("block_table", ctypes.c_void_p),
     ]
 
 
@@ -147,6 +155,10 @@ def lib():
         L.vs_rope_apply.restype = i32
         L.vs_kv_append.argtypes = [ctypes.POINTER(AppendDesc), ctypes.POINTER(RopeDesc)] + [vp] * 13
         L.vs_kv_append.restype = i32
+        L.vs_shared_prefix_workspace_bytes.argtypes = [ctypes.POINTER(AttnDesc), ctypes.POINTER(PrefixDesc)]
+        L.vs_shared_prefix_workspace_bytes.restype = sz
+        L.vs_shared_prefix_attention.argtypes = [ctypes.POINTER(AttnDesc), ctypes.POINTER(PrefixDesc)] + [vp] * 12 + [sz, vp]
+        L.vs_shared_prefix_attention.restype = i32
         L.vs_peak_hbm_read.argtypes = [vp, sz, vp, i32, vp]
         L.vs_peak_hbm_read.restype = i32
         L.vs_peak_hbm_copy.argtypes = [vp, vp, sz, i32, vp]
@@ -195,7 +207,7 @@ def _scalar(code, x):
 _NATIVE = ("vs_tree_mask_build", "vs_tree_verify_attention", "vs_compress_attention", "vs_tree_accept", "vs_tree_accept_noalloc",
            "vs_tree_accept_sample", "vs_draft_expand", "vs_draft_tree_build", "vs_tree_kv_commit")
 # the same for calls that take descriptors of other kinds, or more than one
-_NATIVE_MORE = ("vs_rope_apply", "vs_kv_append")
+_NATIVE_MORE = ("vs_rope_apply", "vs_kv_append", "vs_shared_prefix_attention")
 
 
 def _load_native():
@@ -218,7 +230,7 @@ except ImportError:
     globals().update({name: _missing(name) for name in _NATIVE + _NATIVE_MORE})
 else:
     try:
-        _native.setup(_load_native, _ptr, _scalar, ctypes.byref, ctypes.ArgumentError, AttnDesc, KVDesc, RopeDesc, AppendDesc)
+        _native.setup(_load_native, _ptr, _scalar, ctypes.byref, ctypes.ArgumentError, AttnDesc, KVDesc, RopeDesc, AppendDesc, PrefixDesc)
         globals().update({name: getattr(_native, name) for name in _NATIVE + _NATIVE_MORE})
     except (TypeError, AttributeError):  # built from other sources than these: the package can still be imported to build it
         globals().update({name: _missing(name) for name in _NATIVE + _NATIVE_MORE})
@@ -253,6 +265,10 @@ def vs_attention_workspace_bytes(desc: AttnDesc) -> int:
 
 def vs_compress_attention_workspace_bytes(desc: AttnDesc) -> int:
     return lib().vs_compress_attention_workspace_bytes(ctypes.byref(desc))
+
+
+def vs_shared_prefix_workspace_bytes(desc: AttnDesc, prefix: PrefixDesc) -> int:
+    return lib().vs_shared_prefix_workspace_bytes(ctypes.byref(desc), ctypes.byref(prefix))
 
 
 def vs_accept_workspace_bytes(B: int, T: int, V: int) -> int:

@@ -571,6 +571,51 @@ int32_t accept_chunks(int32_t V) { return (V + kAcceptChunk - 1) / kAcceptChunk;
 
 } // namespace
 
+namespace vs {
+int32_t check_attention(const vs_attn_desc* d, int tree) { return check_desc(d, tree); }
+
+AttnParams attention_params(const vs_attn_desc* desc, int tree, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_len,
+                            const int32_t* tree_parent, const uint64_t* tree_mask, void* out, int32_t* status) {
+    AttnParams p{};
+    p.q = q;
+    p.k = k_cache;
+    p.v = v_cache;
+    p.out = out;
+    p.prefix_len = prefix_len;
+    p.parent = tree_parent;
+    p.tree_mask = tree_mask;
+    p.block_table = desc->paged ? desc->block_table : nullptr;
+    p.status = status;
+    p.B = desc->B;
+    p.T = desc->T;
+    p.tree_keys = tree ? desc->T : 0;
+    p.Hq = desc->Hq;
+    p.Hkv = desc->Hkv;
+    p.d = desc->d;
+    p.group = desc->Hq / desc->Hkv;
+    p.inv_group = 1.f / (float)p.group;
+    p.node_stride = (int64_t)(desc->Hq - p.group) * desc->d;
+    p.row_skip = desc->Hq - p.group;
+    p.rows = p.T * p.group;
+    p.rows_pad = (p.rows + kRowBlock - 1) / kRowBlock * kRowBlock;
+    p.max_prefix_len = desc->max_prefix_len;
+    p.paged = desc->paged ? 1 : 0;
+    p.block_size = desc->paged ? desc->block_size : 1;
+    p.block_shift = 0;
+    while ((1 << p.block_shift) < p.block_size) ++p.block_shift;
+    p.max_blocks = desc->max_blocks;
+    p.num_blocks = desc->num_blocks;
+    p.capacity = desc->capacity;
+    p.stride_seq = desc->stride_seq;
+    p.stride_block = desc->stride_block;
+    p.stride_head = desc->stride_head;
+    p.stride_tok = desc->stride_tok;
+    p.scale = desc->softmax_scale;
+    p.scale_log2 = desc->softmax_scale * 1.4426950408889634f;
+    return p;
+}
+} // namespace vs
+
 extern "C" {
 
 void vs_internal_set_merge_wait(uint32_t ticks) { merge_wait = ticks; }
@@ -664,42 +709,7 @@ int32_t enqueue_attention(const vs_attn_desc* desc, int tree, const void* q, con
         return VS_ERR_WORKSPACE;
     if (const int32_t dc = check_device()) return dc;
 
-    AttnParams p{};
-    p.q = q;
-    p.k = k_cache;
-    p.v = v_cache;
-    p.out = out;
-    p.prefix_len = prefix_len;
-    p.parent = tree_parent;
-    p.tree_mask = tree_mask;
-    p.block_table = desc->paged ? desc->block_table : nullptr;
-    p.status = status;
-    p.B = desc->B;
-    p.T = desc->T;
-    p.tree_keys = tree ? desc->T : 0;
-    p.Hq = desc->Hq;
-    p.Hkv = desc->Hkv;
-    p.d = desc->d;
-    p.group = desc->Hq / desc->Hkv;
-    p.inv_group = 1.f / (float)p.group;
-    p.node_stride = (int64_t)(desc->Hq - p.group) * desc->d;
-    p.row_skip = desc->Hq - p.group;
-    p.rows = pl.rows;
-    p.rows_pad = pl.rows_pad;
-    p.max_prefix_len = desc->max_prefix_len;
-    p.paged = desc->paged ? 1 : 0;
-    p.block_size = desc->paged ? desc->block_size : 1;
-    p.block_shift = 0;
-    while ((1 << p.block_shift) < p.block_size) ++p.block_shift;
-    p.max_blocks = desc->max_blocks;
-    p.num_blocks = desc->num_blocks;
-    p.capacity = desc->capacity;
-    p.stride_seq = desc->stride_seq;
-    p.stride_block = desc->stride_block;
-    p.stride_head = desc->stride_head;
-    p.stride_tok = desc->stride_tok;
-    p.scale = desc->softmax_scale;
-    p.scale_log2 = desc->softmax_scale * 1.4426950408889634f;
+    AttnParams p = attention_params(desc, tree, q, k_cache, v_cache, prefix_len, tree_parent, tree_mask, out, status);
     p.num_splits = pl.num_splits;
     p.keys_per_split = pl.keys_per_split;
     p.row_groups = pl.row_groups;

@@ -1,0 +1,143 @@
+// C-ABI entry point of the attention behind a shared prefix: host-side checks, launch planning and enqueues.
+#include "vs_internal.h"
+
+namespace {
+
+using namespace vs;
+
+constexpr size_t kAlign = 256;
+inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+constexpr int64_t kMaxSharedRows = 1 << 20; // of a KV head: node_of_row_short() is exact up to 2^21, and a partial result of this many rows is 512 MB
+
+// The shared prefix as the cache of one sequence, all sequences' nodes its queries.
+vs_attn_desc prefix_as_desc(const vs_attn_desc* d, const vs_prefix_desc* x) {
+    vs_attn_desc s = *d;
+    s.B = 1;
+    s.T = 1; // (set to B * T behind the checks)
+    s.max_prefix_len = x->max_len;
+    s.paged = x->paged;
+    s.block_size = x->block_size;
+    s.max_blocks = x->max_blocks;
+    s.num_blocks = x->num_blocks;
+    s.capacity = x->capacity;
+    s.stride_seq = 0;
+    s.stride_block = x->stride_block;
+    s.stride_head = x->stride_head;
+    s.stride_tok = x->stride_tok;
+    s.block_table = x->block_table;
+    return s;
+}
+
+int32_t check_shared(const vs_attn_desc* d, const vs_prefix_desc* x, vs_attn_desc& prefix) {
+    if (!d || !x) return VS_ERR_NULL;
+    if (d->impl != VS_IMPL_AUTO || d->num_splits != 0 || d->rows_per_wave != 0 || d->waves_per_group != 0 || d->schedule != VS_SCHED_AUTO)
+        return VS_ERR_SHAPE;
+    if (const int32_t rc = check_attention(d, 1)) return rc;
+    if ((int64_t)d->B * d->T * (d->Hq / d->Hkv) > kMaxSharedRows) return VS_ERR_SHAPE;
+    prefix = prefix_as_desc(d, x);
+    if (const int32_t rc = check_attention(&prefix, 0)) return rc;
+    prefix.T = d->B * d->T;
+    return VS_OK;
+}
+
+// A launch of the shared keys, or of the sequences' own.
+struct Cut {
+    int32_t rows_per_group, row_groups, num_splits, keys_per_split, total_wgs;
+};
+struct SharedPlan {
+    Cut shared, own;
+    size_t acc_bytes, ml_bytes;
+};
+
+SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
+    SharedPlan pl{};
+    const int group = d->Hq / d->Hkv;
+    const int64_t rows = (int64_t)d->B * d->T * group;
+    const bool f32 = d->dtype == VS_F32;
+    const int tiles = (prefix.max_prefix_len + kIterKeys - 1) / kIterKeys;
+    Cut& s = pl.shared;
+    s.rows_per_group = f32 ? 8 : d->d == 128 && rows > kRowBlock ? 2 * kRowBlock : kRowBlock;
+    s.row_groups = (int32_t)((rows + s.rows_per_group - 1) / s.rows_per_group);
+    const int64_t wgs = (int64_t)d->Hkv * s.row_groups;
+    int64_t splits = kNumCUs / wgs;
+    if (splits > (tiles + 3) / 4) splits = (tiles + 3) / 4;
+    if (splits > kMergeMaxSplits) splits = kMergeMaxSplits;
+    if (splits < 1) splits = 1;
+    const int tps = (int)((tiles + splits - 1) / splits);
+    s.keys_per_split = tps * kIterKeys;
+    s.num_splits = (tiles + tps - 1) / tps;
+    s.total_wgs = (int32_t)(wgs * s.num_splits);
+    Cut& o = pl.own;
+    const int own_rows = d->T * group;
+    o.rows_per_group = f32 ? ((int64_t)d->B * d->Hkv * ((own_rows + 3) / 4) <= kNumCUs ? 4 : 8) : d->d == 128 && own_rows > kRowBlock ? 2 * kRowBlock : kRowBlock;
+    o.row_groups = (own_rows + o.rows_per_group - 1) / o.rows_per_group;
+    o.num_splits = 1;
+    o.keys_per_split = (int32_t)(((int64_t)d->max_prefix_len + d->T + kIterKeys - 1) / kIterKeys * kIterKeys);
+    o.total_wgs = d->B * d->Hkv * o.row_groups;
+    const size_t partial = (size_t)d->Hkv * s.num_splits * rows;
+    pl.acc_bytes = align_up(partial * d->d * sizeof(float));
+    pl.ml_bytes = align_up(partial * 2 * sizeof(float));
+    return pl;
+}
+
+SharedParams shared_params(const AttnParams& base, const Cut& c, const SharedPlan& pl, const vs_attn_desc* d, const vs_attn_desc& prefix, const int32_t* shared_len,
+                           void* workspace) {
+    SharedParams p{};
+    (AttnParams&)p = base;
+    p.rows_per_group = c.rows_per_group;
+    p.row_groups = c.row_groups;
+    p.num_splits = c.num_splits;
+    p.keys_per_split = c.keys_per_split;
+    p.total_wgs = c.total_wgs;
+    p.by_splits = fast_div_by(c.num_splits);
+    p.by_groups = fast_div_by(c.row_groups);
+    p.by_heads = fast_div_by(d->Hkv);
+    p.sh_acc = (float*)workspace;
+    p.sh_ml = (float*)((char*)workspace + pl.acc_bytes);
+    p.shared_len = shared_len;
+    p.shared_table = prefix.paged ? prefix.block_table : nullptr;
+    p.sh_rows = d->B * d->T * (d->Hq / d->Hkv);
+    p.sh_splits = pl.shared.num_splits;
+    p.sh_keys_per_split = pl.shared.keys_per_split;
+    p.max_shared = prefix.max_prefix_len;
+    while (prefix.paged && (1 << p.sh_block_shift) < prefix.block_size) ++p.sh_block_shift;
+    p.sh_num_blocks = prefix.num_blocks;
+    p.sh_slots = prefix.paged ? (int64_t)prefix.max_blocks * prefix.block_size : prefix.capacity;
+    return p;
+}
+
+} // namespace
+
+extern "C" {
+
+size_t vs_shared_prefix_workspace_bytes(const vs_attn_desc* desc, const vs_prefix_desc* prefix) {
+    vs_attn_desc x;
+    if (check_shared(desc, prefix, x) != VS_OK) return 0;
+    const SharedPlan pl = plan_shared(desc, x);
+    return pl.acc_bytes + pl.ml_bytes;
+}
+
+int32_t vs_shared_prefix_attention(const vs_attn_desc* desc, const vs_prefix_desc* prefix, const void* q, const void* k_shared, const void* v_shared,
+                                   const int32_t* shared_len, const void* k_cache, const void* v_cache, const int32_t* prefix_len,
+                                   const int32_t* tree_parent, const uint64_t* tree_mask, void* out, int32_t* status, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+    if (!desc || !prefix || !q || !k_shared || !v_shared || !shared_len || !k_cache || !v_cache || !prefix_len || !tree_parent || !out) return VS_ERR_NULL;
+    vs_attn_desc x;
+    if (const int32_t rc = check_shared(desc, prefix, x)) return rc;
+    for (const void* at : {q, k_shared, v_shared, k_cache, v_cache, (const void*)out})
+        if (!aligned16(at)) return VS_ERR_LAYOUT;
+    const SharedPlan pl = plan_shared(desc, x);
+    if (!workspace || workspace_bytes < pl.acc_bytes + pl.ml_bytes || ((uintptr_t)workspace & (kAlign - 1))) return VS_ERR_WORKSPACE;
+    if (const int32_t dc = check_device()) return dc;
+    hipStream_t s = (hipStream_t)stream;
+    const bool f32 = desc->dtype == VS_F32;
+    const SharedParams first = shared_params(attention_params(&x, 0, q, k_shared, v_shared, shared_len, nullptr, nullptr, nullptr, nullptr), pl.shared, pl, desc, x,
+                                             shared_len, workspace);
+    const SharedParams second = shared_params(attention_params(desc, 1, q, k_cache, v_cache, prefix_len, tree_parent, tree_mask, out, status), pl.own, pl, desc, x,
+                                              shared_len, workspace);
+    hipError_t e = f32 ? launch_attention_shared_f32(first, kRowsShared, s) : launch_attention_shared_rows(first, kRowsShared, s);
+    if (e == hipSuccess) e = f32 ? launch_attention_shared_f32(second, kRowsOwn, s) : launch_attention_shared_rows(second, kRowsOwn, s);
+    return e == hipSuccess ? VS_OK : VS_ERR_HIP;
+}
+
+} // extern "C"

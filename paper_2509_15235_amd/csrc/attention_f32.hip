@@ -21,7 +21,7 @@
 // that would be idle otherwise (the host's choice).
 // Before (one wave per row, plain fused multiply-adds): 2 x 31 nodes, 8 / 2 heads of 128 channels, 333 - 600
 // keys 188 us; 8 nodes over 64 keys, 4 / 1 heads of 64 channels 19 us. Now 10.6 and 4.7 us.
-#include "attn_mfma_common.h"
+#include "attn_shared.h"
 
 namespace vs {
 
@@ -53,8 +53,9 @@ __device__ __forceinline__ float row_all(float x, Op op) {
     return op(__uint_as_float(w[0]), __uint_as_float(w[1]));
 }
 
-template <int D, int SETS, bool PAGED>
-__global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const AttnParams p) {
+// MODE: as in attention_mfma_rows.hip. kRowsShared has key splits: of the keys that all sequences share each takes keys_per_split.
+template <int D, int SETS, bool PAGED, int MODE = kRowsWhole>
+__global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const std::conditional_t<MODE == kRowsWhole, AttnParams, SharedParams> p) {
     request_args(p);
     constexpr int KJ = D / 16; // 16-byte pieces of a key row per lane
     constexpr int VM = D / 64; // ... of a value row
@@ -67,6 +68,7 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
     __shared__ float sm[SETS][PARTS][4], sl[SETS][PARTS][4];             // references and sums
     __shared__ int32_t sp[VS_MAX_TREE];
     __shared__ int32_t sflag;
+    __shared__ f32x2 row_ml[MODE == kRowsWhole ? 1 : ROWS]; // references and sums of the rows
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -76,6 +78,7 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
     const WorkItem at = work_item(p);
     if (at.none) return;
     const int rg = at.rg, kvh = at.kvh, b = at.b;
+    const int first = (MODE == kRowsShared ? at.split * p.keys_per_split : 0) + kF32Tile * wave; // this wave's first tile
 
     const int32_t S = p.prefix_len[b]; // requested first; the first tile and the queries do not wait for it
     const int64_t cache_tokens = PAGED ? (int64_t)p.max_blocks * p.block_size : p.capacity;
@@ -134,7 +137,7 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
                     vf[r][m] = *(const f32x4*)(vbase + base + (int64_t)min(4 * kb + r, lim) * p.stride_tok + 64 * m + 4 * (lane & 15));
         }
     };
-    load_k(kF32Tile * wave, last_slot);
+    load_k(first, last_slot);
 
     // queries: set s, row rg * 8 + 4 s + j; rows past the end repeat the last one (results discarded)
     f32x4 qf[SETS][KJ];
@@ -152,7 +155,7 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
     const bool given = p.tree_mask && p.tree_keys != 0;
 #pragma unroll
     for (int s = 0; s < SETS; ++s) mask[s] = given ? p.tree_mask[(int64_t)b * p.T + node[s]] : 0ull;
-    load_v(kF32Tile * wave, last_slot);
+    load_v(first, last_slot);
 
     int32_t tree_code = VS_STATUS_OK;
     if (p.tree_mask || p.tree_keys == 0) {
@@ -163,6 +166,8 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
     }
     const bool s_ok = prefix_ok(p, S);
     if (kvh == 0 && rg == 0) report_status(p, b, tree_code, s_ok, S, &sflag);
+    if constexpr (MODE == kRowsOwn)
+        if (kvh == 0 && rg == 0) report_shared(p, b, &sflag);
     if (tree_code != VS_STATUS_OK || !s_ok) return;
     if (!given && p.tree_keys != 0) {
 #pragma unroll
@@ -170,6 +175,11 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
     }
 
     const int n = S + p.tree_keys;
+    int end = n; // of this workgroup's keys
+    if constexpr (MODE == kRowsShared) {
+        if (at.split * p.keys_per_split >= n) return;
+        end = min(n, (at.split + 1) * p.keys_per_split);
+    }
     float m2[SETS], l[SETS]; // reference (log2 domain, scaled) and sum of this lane's key group and row
     f32x4 acc[SETS][VM][4];
 #pragma unroll
@@ -182,7 +192,7 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
             for (int e = 0; e < 4; ++e) acc[s][m][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    for (int t0 = kF32Tile * wave; t0 < n; t0 += kF32Tile * kF32Waves) {
+    for (int t0 = first; t0 < end; t0 += kF32Tile * kF32Waves) {
         f32x4 sc[SETS][2]; // two chains per set
 #pragma unroll
         for (int s = 0; s < SETS; ++s)
@@ -196,7 +206,7 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
             const int r = KPI * i + krow;
             *(f32x4*)(sk[wave] + r * D + 4 * (kchunk ^ (4 * (r & 3)))) = kf[i];
         }
-        if (SETS == 1 && t0 + kF32Tile * kF32Waves < n) load_k(t0 + kF32Tile * kF32Waves, n - 1);
+        if (SETS == 1 && t0 + kF32Tile * kF32Waves < end) load_k(t0 + kF32Tile * kF32Waves, n - 1);
         f32x4 ka[KJ];
 #pragma unroll
         for (int i = 0; i < KJ; ++i) ka[i] = *(const f32x4*)(sk[wave] + (4 * kb + j) * D + 4 * ((4 * i + cg) ^ (4 * j)));
@@ -209,7 +219,7 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
                     sc[s][e & 1] = __builtin_amdgcn_mfma_f32_4x4x1f32(ka[i][e], qf[s][i][e], sc[s][e & 1], 0, 0, 0);
 
         // (two sets: the registers of the next tile are free only now)
-        if (SETS == 2 && t0 + kF32Tile * kF32Waves < n) load_k(t0 + kF32Tile * kF32Waves, n - 1);
+        if (SETS == 2 && t0 + kF32Tile * kF32Waves < end) load_k(t0 + kF32Tile * kF32Waves, n - 1);
 
         float pr[SETS][4];
 #pragma unroll
@@ -302,7 +312,7 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
 #pragma unroll
                     for (int s = 0; s < SETS; ++s)
                         acc[s][m][e] = __builtin_amdgcn_mfma_f32_4x4x1f32(vf[r][m][e], pr[s][r], acc[s][m][e], 0, 0, 0);
-        if (t0 + kF32Tile * kF32Waves < n) load_v(t0 + kF32Tile * kF32Waves, n - 1);
+        if (t0 + kF32Tile * kF32Waves < end) load_v(t0 + kF32Tile * kF32Waves, n - 1);
     }
 
     // ---- merge the key groups of all waves (log-sum-exp): everybody scales by the common reference and
@@ -323,7 +333,8 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
         float M = row_all(fmaxf(ma, mb), [](float x, float y) { return fmaxf(x, y); }); // finite: a node sees itself or the prefix
         const float den = row_all(sl[s][q][j] * __builtin_amdgcn_exp2f(ma - M) + sl[s][q + 1][j] * __builtin_amdgcn_exp2f(mb - M),
                                   [](float x, float y) { return x + y; });
-        const float f = __builtin_amdgcn_exp2f(m2[s] - M) / den;
+        const float f = MODE == kRowsWhole ? __builtin_amdgcn_exp2f(m2[s] - M) / den : __builtin_amdgcn_exp2f(m2[s] - M);
+        if constexpr (MODE != kRowsWhole) row_ml[4 * s + j] = f32x2{M, den}; // (the same from all lanes of a row)
         // registers in the order of their channels: 16 VM of them, halved twice
         float x[16 * VM];
 #pragma unroll
@@ -362,6 +373,27 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const At
         for (int w = 0; w < kF32Waves; ++w) // waves without a tile hold zeros
 #pragma unroll
             for (int e = 0; e < CPT; ++e) o[e] += so[(w * ROWS + row) * PITCH + c + e];
+        if constexpr (MODE == kRowsShared) {
+            const int64_t to = shared_row(p, kvh, at.split, r);
+#pragma unroll
+            for (int e = 0; e < CPT; ++e) p.sh_acc[to * D + c + e] = o[e];
+            if (c == 0) *(f32x2*)(p.sh_ml + to * 2) = row_ml[row];
+            return;
+        } else if constexpr (MODE == kRowsOwn) {
+            const int parts = shared_parts(p);
+            float m = row_ml[row][0], l = row_ml[row][1];
+            for (int s = 0; s < parts; ++s) {
+                const int64_t from = shared_row(p, kvh, s, b * p.rows + r);
+                const f32x2 ml = *(const f32x2*)(p.sh_ml + from * 2);
+                const float M = fmaxf(m, ml[0]), f = __builtin_amdgcn_exp2f(m - M), g = __builtin_amdgcn_exp2f(ml[0] - M);
+                l = l * f + ml[1] * g;
+                m = M;
+#pragma unroll
+                for (int e = 0; e < CPT; ++e) o[e] = o[e] * f + p.sh_acc[from * D + c + e] * g;
+            }
+#pragma unroll
+            for (int e = 0; e < CPT; ++e) o[e] /= l;
+        }
         float* dst = (float*)p.out + row_start<D>(p, b, kvh) + (uint64_t)row_number(r, row_node(p, r), p.row_skip) * (uint32_t)D + c;
 #pragma unroll
         for (int e = 0; e < CPT; ++e) dst[e] = o[e];
@@ -376,7 +408,27 @@ hipError_t launch_f32(const AttnParams& p, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <int D, int SETS, int MODE>
+void launch_f32_shared(const SharedParams& p, hipStream_t s) {
+    const dim3 grid((p.total_wgs + 7) / 8 * 8), block(kF32Waves * kWave);
+    if (p.paged) hipLaunchKernelGGL((attn_f32_kernel<D, SETS, true, MODE>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((attn_f32_kernel<D, SETS, false, MODE>), grid, block, 0, s, p);
+}
+template <int MODE>
+void launch_f32_shared(const SharedParams& p, hipStream_t s) {
+    if (p.rows_per_group == 4) p.d == 128 ? launch_f32_shared<128, 1, MODE>(p, s) : launch_f32_shared<64, 1, MODE>(p, s);
+    else p.d == 128 ? launch_f32_shared<128, 2, MODE>(p, s) : launch_f32_shared<64, 2, MODE>(p, s);
+}
+
 } // namespace
+
+hipError_t launch_attention_shared_f32(const SharedParams& p, RowsMode mode, hipStream_t s) {
+    if ((p.rows_per_group != 4 && p.rows_per_group != 8) || p.row_groups * p.rows_per_group < p.rows || (p.d != 64 && p.d != 128)) return hipErrorInvalidValue;
+    if (p.keys_per_split % kF32Tile || (mode == kRowsOwn && p.num_splits != 1)) return hipErrorInvalidValue;
+    if (mode == kRowsShared) launch_f32_shared<kRowsShared>(p, s);
+    else launch_f32_shared<kRowsOwn>(p, s);
+    return hipGetLastError();
+}
 
 hipError_t launch_attention_f32(const AttnParams& p, hipStream_t s) {
     if (p.rows_per_group == 4) return p.d == 128 ? launch_f32<128, 1>(p, s) : launch_f32<64, 1>(p, s);

@@ -20,7 +20,7 @@
 // (Three and four row blocks, one wave per SIMD with 512 registers, lost: 16 x 13 nodes, up to 8191 keys 57 / 79.)
 #include <type_traits>
 
-#include "attn_mfma_common.h"
+#include "attn_shared.h"
 
 namespace vs {
 
@@ -31,8 +31,10 @@ namespace {
 // ONCE: tiles as data that is read once (the host's rule says when). Part of the kernel as well: a branch at every load 5 % of two row blocks'
 // time, a loop of its own for either kind 3 % of a short call's.
 // CROWD: many splits on nearly all CUs, whose workgroups wait for each other at another word (merge_meet).
-template <int D, int NW, int RB, bool PAGED, bool ONCE, bool CROWD = false>
-__global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const AttnParams p) {
+// MODE: kRowsShared, all sequences' rows against the keys that they share (one sequence of B * T nodes, no tree slots), whose results stay
+// partial ones in fp32; kRowsOwn, a sequence's rows against its own keys, joined with those (attn_shared.h).
+template <int D, int NW, int RB, bool PAGED, bool ONCE, bool CROWD = false, int MODE = kRowsWhole>
+__global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::conditional_t<MODE == kRowsWhole, AttnParams, SharedParams> p) {
     constexpr int KS = D / 16;          // k-steps of the S^T product
     constexpr int DB = D / 32;          // 32-channel blocks of the output
     constexpr int SUB = kTileKeys * D;  // elements per 32-key tile of K (or V)
@@ -159,9 +161,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const AttnPa
         mask[rb] = p.tree_mask && p.tree_keys != 0 ? p.tree_mask[(int64_t)b * p.T + node[rb]] : 0ull;
     }
     // the gate of the (sequence, KV head), opened below
-    uint64_t* const gate = p.gates ? p.gates + kGateWords * ((int64_t)unit * p.row_groups + rg) : nullptr;
+    uint64_t* const gate = MODE == kRowsWhole && p.gates ? p.gates + kGateWords * ((int64_t)unit * p.row_groups + rg) : nullptr;
     uint64_t seen = 0;
-    if (p.gates && wave == 0) seen = gate_load(gate);
+    if (MODE == kRowsWhole && p.gates && wave == 0) seen = gate_load(gate);
     if (first < kend) { // uniform per wave
         issue(std::false_type{}, sK, first, kend - 1);
         issue(std::true_type{}, sV, first, kend - 1);
@@ -180,11 +182,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const AttnPa
     }
     const bool s_ok = prefix_ok(p, S);
     if (kvh == 0 && split == 0 && rg == 0) report_status<PAGED>(p, b, tree_code, s_ok, S, &sflag);
+    if constexpr (MODE == kRowsOwn)
+        if (kvh == 0 && rg == 0) report_shared(p, b, &sflag);
     if (tree_code != VS_STATUS_OK || !s_ok) return;
     const int nk = S + p.tree_keys;
     if (k0 >= nk) return;
-    const bool final_rows = p.num_splits == 1 || (p.gates && nk <= p.keys_per_split); // a sequence of one split has nothing to merge
-    const bool merge = p.gates && !final_rows;
+    const bool final_rows = MODE == kRowsOwn || p.num_splits == 1 || (p.gates && nk <= p.keys_per_split); // a sequence of one split has nothing to merge
+    const bool merge = MODE == kRowsWhole && p.gates && !final_rows;
     if (merge && tid == 0) [[unlikely]] merge_open(gate, seen); // (most waves only jump over it)
     const int k1 = min(nk, k0 + p.keys_per_split);
 
@@ -325,6 +329,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const AttnPa
         }
     }
     wait_loads<0>(); // (a wave without a live tile may have requested one)
+    int parts = 0;
+    if constexpr (MODE == kRowsOwn) parts = shared_parts(p);
 
     // ---- merge the waves' results through LDS (log-sum-exp) and write the rows. The accumulators are NP pieces of eight
     // registers (piece = channel block * 2 + half of its registers, the 16-byte unit of the partial-result layout):
@@ -383,7 +389,34 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const AttnPa
                 }
             }
             const float l = half_sum(lall);
-            const float inv = l > 0.f ? 1.f / l : 0.f; // no visible key in this split (partials only): zeros, weight 0
+            float inv = l > 0.f ? 1.f / l : 0.f; // no visible key in this split (partials only): zeros, weight 0
+            if constexpr (MODE != kRowsWhole) {
+                const int row = row0 + rb * kRowBlock + col;
+                f32x4 o[2 * PPW]; // channels at(i) .. + 3 of the lane's row
+                auto at = [&](int i) __attribute__((always_inline)) { return (wave * PPW + (i >> 1)) * 16 + (i & 1) * 8 + 4 * half; };
+#pragma unroll
+                for (int i = 0; i < PPW; ++i) {
+                    o[2 * i] = f32x4{r[i][0], r[i][1], r[i][2], r[i][3]};
+                    o[2 * i + 1] = f32x4{r[i][4], r[i][5], r[i][6], r[i][7]};
+                }
+                if constexpr (MODE == kRowsShared) {
+                    if (row >= p.rows) continue;
+                    const int64_t to = shared_row(p, kvh, split, row);
+#pragma unroll
+                    for (int i = 0; i < 2 * PPW; ++i) *(f32x4*)(p.sh_acc + to * D + at(i)) = o[i];
+                    if (wave == 0 && half == 0) *(f32x2*)(p.sh_ml + to * 2) = f32x2{M, l};
+                    continue;
+                } else {
+                    inv = join_shared<D>(p, kvh, b * p.rows + min(row, p.rows - 1), parts, M, l, o, at);
+#pragma unroll
+                    for (int i = 0; i < PPW; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            r[i][e] = o[2 * i][e];
+                            r[i][4 + e] = o[2 * i + 1][e];
+                        }
+                }
+            }
 #pragma unroll
             for (int i = 0; i < PPW; ++i) {
                 const int pc = wave * PPW + i;
@@ -410,7 +443,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const AttnPa
             }
         }
     }
-    if (merge) merge_splits<D, CROWD>(p, gate, b, kvh, block0, block0 + RB, split, (nk + p.keys_per_split - 1) / p.keys_per_split, NW, (uint32_t*)sp);
+    if constexpr (MODE == kRowsWhole)
+        if (merge) merge_splits<D, CROWD>(p, gate, b, kvh, block0, block0 + RB, split, (nk + p.keys_per_split - 1) / p.keys_per_split, NW, (uint32_t*)sp);
 }
 
 template <int D, int NW, int RB>
@@ -429,7 +463,27 @@ hipError_t launch_rows(const AttnParams& p, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <int D, int RB, int MODE>
+hipError_t launch_shared(const SharedParams& p, hipStream_t s) {
+    const dim3 grid(((p.total_wgs + 7) / 8) * 8), block(8 * kWave);
+    if (p.paged) hipLaunchKernelGGL((attn_mfma_rows_kernel<D, 8, RB, true, false, false, MODE>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((attn_mfma_rows_kernel<D, 8, RB, false, false, false, MODE>), grid, block, 0, s, p);
+    return hipGetLastError();
+}
+template <int MODE>
+hipError_t launch_shared(const SharedParams& p, int blocks, hipStream_t s) {
+    if (p.d == 128) return blocks == 2 ? launch_shared<128, 2, MODE>(p, s) : launch_shared<128, 1, MODE>(p, s);
+    return launch_shared<64, 1, MODE>(p, s);
+}
+
 } // namespace
+
+hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, hipStream_t s) {
+    const int blocks = p.rows_per_group / kRowBlock;
+    if (p.row_groups * p.rows_per_group < p.rows || (p.d != 64 && p.d != 128) || blocks < 1 || blocks > (p.d == 128 ? 2 : 1)) return hipErrorInvalidValue;
+    if (p.keys_per_split % kIterKeys || (mode == kRowsOwn && p.num_splits != 1)) return hipErrorInvalidValue;
+    return mode == kRowsShared ? launch_shared<kRowsShared>(p, blocks, s) : launch_shared<kRowsOwn>(p, blocks, s);
+}
 
 // One row block and four or eight waves; with 128 channels also two row blocks and eight waves.
 bool attention_rows_supported(int d, int row_blocks, int waves) {

@@ -20,7 +20,7 @@
 
 namespace {
 
-PyObject *s_data_ptr, *g_load, *g_ptr, *g_scalar, *g_struct, *g_error, *g_attn_desc, *g_kv_desc, *g_rope_desc, *g_append_desc; // setup()
+PyObject *s_data_ptr, *g_load, *g_ptr, *g_scalar, *g_struct, *g_error, *g_attn_desc, *g_kv_desc, *g_rope_desc, *g_append_desc, *g_prefix_desc; // setup()
 
 constexpr int kMaxArgs = 20;
 struct Entry {
@@ -156,6 +156,12 @@ bool convert(PyObject* o, int i, const vs_append_desc*& x) {
     x = (const vs_append_desc*)v;
     return true;
 }
+bool convert(PyObject* o, int i, const vs_prefix_desc*& x) {
+    uint64_t v;
+    if (!to_struct(o, i, g_prefix_desc, sizeof(vs_prefix_desc), v)) return false;
+    x = (const vs_prefix_desc*)v;
+    return true;
+}
 template <typename T>
 bool convert(PyObject* o, int i, T*& x) {
     uint64_t v;
@@ -235,6 +241,8 @@ Entry entries[] = {
     {"vs_tree_kv_commit", "desc k_cache v_cache prefix_len path accepted_len new_prefix_len status stream", 7},
     {"vs_rope_apply", "rope x x_stride_row x_stride_head positions rows H d dtype out out_stride_row out_stride_head stream", 12},
     {"vs_kv_append", "desc rope q k v positions depth pos_offset prefix_len row_start q_out k_cache v_cache status stream", 13},
+    {"vs_shared_prefix_attention",
+     "desc prefix q k_shared v_shared shared_len k_cache v_cache prefix_len tree_parent tree_mask out status workspace workspace_bytes stream", 12},
 };
 
 #define VS_ENTRY(INDEX, NAME)                                                                       \
@@ -253,13 +261,14 @@ VS_ENTRY(7, vs_draft_tree_build)
 VS_ENTRY(8, vs_tree_kv_commit)
 VS_ENTRY(9, vs_rope_apply)
 VS_ENTRY(10, vs_kv_append)
+VS_ENTRY(11, vs_shared_prefix_attention)
 
-// setup(load, ptr, scalar, byref, ArgumentError, AttnDesc, KVDesc, RopeDesc, AppendDesc)
+// setup(load, ptr, scalar, byref, ArgumentError, AttnDesc, KVDesc, RopeDesc, AppendDesc, PrefixDesc)
 PyObject* setup(PyObject*, PyObject* args) {
-    if (!PyArg_ParseTuple(args, "OOOOOO!O!O!O!", &g_load, &g_ptr, &g_scalar, &g_struct, &g_error, &PyType_Type, &g_attn_desc, &PyType_Type, &g_kv_desc,
-                          &PyType_Type, &g_rope_desc, &PyType_Type, &g_append_desc))
+    if (!PyArg_ParseTuple(args, "OOOOOO!O!O!O!O!", &g_load, &g_ptr, &g_scalar, &g_struct, &g_error, &PyType_Type, &g_attn_desc, &PyType_Type, &g_kv_desc,
+                          &PyType_Type, &g_rope_desc, &PyType_Type, &g_append_desc, &PyType_Type, &g_prefix_desc))
         return nullptr;
-    for (PyObject* o : {g_load, g_ptr, g_scalar, g_struct, g_error, g_attn_desc, g_kv_desc, g_rope_desc, g_append_desc}) Py_INCREF(o); // for good
+    for (PyObject* o : {g_load, g_ptr, g_scalar, g_struct, g_error, g_attn_desc, g_kv_desc, g_rope_desc, g_append_desc, g_prefix_desc}) Py_INCREF(o); // for good
     Py_RETURN_NONE;
 }
 // bind({name: address}): the calls that it names
@@ -282,7 +291,7 @@ PyObject* bind(PyObject*, PyObject* addresses) {
 PyMethodDef methods[] = {
     VS_METHOD(vs_tree_mask_build), VS_METHOD(vs_tree_verify_attention), VS_METHOD(vs_compress_attention), VS_METHOD(vs_tree_accept),
     VS_METHOD(vs_tree_accept_noalloc), VS_METHOD(vs_tree_accept_sample), VS_METHOD(vs_draft_expand), VS_METHOD(vs_draft_tree_build),
-    VS_METHOD(vs_tree_kv_commit), VS_METHOD(vs_rope_apply), VS_METHOD(vs_kv_append),
+    VS_METHOD(vs_tree_kv_commit), VS_METHOD(vs_rope_apply), VS_METHOD(vs_kv_append), VS_METHOD(vs_shared_prefix_attention),
     {"setup", setup, METH_VARARGS, nullptr},
     {"bind", bind, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},

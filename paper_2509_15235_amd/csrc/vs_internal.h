@@ -83,6 +83,21 @@ struct AttnParams {
     FastDiv bal_per_seq;        // bal_chunks / B where that is whole; else d = 0
 };
 
+// Attention of a batch behind one shared prefix, in two launches: all sequences' rows against the shared keys, whose partial results stay
+// in fp32, and every sequence's rows against its own keys, joined with them.
+enum RowsMode { kRowsWhole = 0, kRowsShared = 1, kRowsOwn = 2 }; // the kernels of vs_tree_verify_attention, and these two
+struct SharedParams : AttnParams {
+    float* sh_acc;              // [KV head][split][row][d]: sums of weights times values, relative to the split's reference
+    float* sh_ml;               // [KV head][split][row][2]: reference (log2 domain), sum of weights
+    const int32_t* shared_len;
+    const int32_t* shared_table; // paged only
+    int32_t sh_rows;            // rows of all sequences: B * T * group
+    int32_t sh_splits, sh_keys_per_split;
+    int32_t max_shared;
+    int32_t sh_block_shift, sh_num_blocks; // paged only
+    int64_t sh_slots;           // of the shared prefix's cache
+};
+
 struct AcceptParams {
     const float* logits;
     int64_t ld;
@@ -247,6 +262,10 @@ extern "C" int32_t vs_internal_reads_once(const vs_attn_desc* desc, int32_t tree
 
 inline bool is_pow2(int32_t x) { return x > 0 && (x & (x - 1)) == 0; }
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+int32_t check_attention(const vs_attn_desc* d, int tree); // shapes, types and layouts that need no device (api.hip)
+// What a descriptor says, as the kernels take it; the plan's numbers are left at zero (api.hip)
+AttnParams attention_params(const vs_attn_desc* d, int tree, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_len,
+                            const int32_t* tree_parent, const uint64_t* tree_mask, void* out, int32_t* status);
 int32_t check_device(); // VS_OK when the current device is a gfx950, else VS_ERR_NO_DEVICE (api.hip)
 
 hipError_t launch_tree_mask(const int32_t* parent, int32_t B, int32_t T, uint64_t* mask,
@@ -262,6 +281,8 @@ bool attention_resident_supported(int row_blocks);
 hipError_t launch_attention_mfma_resident(const AttnParams& p, int row_blocks, hipStream_t s);
 hipError_t launch_attention_mfma_rows(const AttnParams& p, int waves, hipStream_t s);
 hipError_t launch_attention_mfma_rounds(const AttnParams& p, int row_blocks, hipStream_t s);
+hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, hipStream_t s);
+hipError_t launch_attention_shared_f32(const SharedParams& p, RowsMode mode, hipStream_t s);
 hipError_t launch_attention_combine(const AttnParams& p, int dtype, hipStream_t s);
 hipError_t launch_accept(AcceptParams p, void* workspace, hipStream_t s);        // sets pairs, chunks
 hipError_t launch_accept_sample(SampleParams p, void* workspace, hipStream_t s); // likewise
