@@ -1,4 +1,5 @@
 // C-ABI entry point of the attention behind a shared prefix: host-side checks, launch planning and enqueues.
+#include <stdlib.h>
 #include "vs_internal.h"
 
 namespace {
@@ -46,6 +47,8 @@ struct Cut {
 };
 struct SharedPlan {
     Cut shared, own;
+    int32_t own_waves, own_pipe;
+    int32_t waves, shares; // the pipelined kernel on equal shares of all row groups' keys; 0: own tiles, equal splits
     size_t acc_bytes, ml_bytes;
 };
 
@@ -56,6 +59,18 @@ SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
     const bool f32 = d->dtype == VS_F32;
     const int tiles = (prefix.max_prefix_len + kIterKeys - 1) / kIterKeys;
     Cut& s = pl.shared;
+    if (!f32 && rows > (getenv("PIPEROWS") ? atoi(getenv("PIPEROWS")) : 128)) {
+        pl.waves = getenv("W4") ? 4 : 8;
+        s.rows_per_group = pl.waves * kRowBlock;
+        s.row_groups = (int32_t)((rows + s.rows_per_group - 1) / s.rows_per_group);
+        const int64_t units = (int64_t)d->Hkv * s.row_groups, steps = units * tiles, places = kNumCUs * (pl.waves == 8 ? 1 : 2);
+        pl.shares = (int32_t)(steps / 4 < places ? (steps + 3) / 4 : places);
+        if (pl.shares < units && pl.shares < places) pl.shares = (int32_t)(units < places ? units : places);
+        // a unit's steps begin in one share and end in another: at most so many
+        s.num_splits = (int32_t)((pl.shares + units - 1) / units) + 1;
+        s.keys_per_split = kIterKeys;
+        s.total_wgs = pl.shares;
+    } else {
     s.rows_per_group = f32 ? 8 : d->d == 128 && rows > kRowBlock ? 2 * kRowBlock : kRowBlock;
     s.row_groups = (int32_t)((rows + s.rows_per_group - 1) / s.rows_per_group);
     const int64_t wgs = (int64_t)d->Hkv * s.row_groups;
@@ -67,16 +82,24 @@ SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
     s.keys_per_split = tps * kIterKeys;
     s.num_splits = (tiles + tps - 1) / tps;
     s.total_wgs = (int32_t)(wgs * s.num_splits);
+    }
     Cut& o = pl.own;
     const int own_rows = d->T * group;
     o.rows_per_group = f32 ? ((int64_t)d->B * d->Hkv * ((own_rows + 3) / 4) <= kNumCUs ? 4 : 8) : d->d == 128 && own_rows > kRowBlock ? 2 * kRowBlock : kRowBlock;
+    if (!f32 && own_rows > 2 * kRowBlock) {
+        pl.own_pipe = 1;
+        pl.own_waves = getenv("OWN8") ? 8 : 4;
+        o.rows_per_group = pl.own_waves * kRowBlock;
+    }
     o.row_groups = (own_rows + o.rows_per_group - 1) / o.rows_per_group;
     o.num_splits = 1;
     o.keys_per_split = (int32_t)(((int64_t)d->max_prefix_len + d->T + kIterKeys - 1) / kIterKeys * kIterKeys);
     o.total_wgs = d->B * d->Hkv * o.row_groups;
-    const size_t partial = (size_t)d->Hkv * s.num_splits * rows;
-    pl.acc_bytes = align_up(partial * d->d * sizeof(float));
-    pl.ml_bytes = align_up(partial * 2 * sizeof(float));
+    if (!pl.own_pipe) pl.own_waves = o.rows_per_group > kRowBlock || o.total_wgs <= kNumCUs ? 8 : o.total_wgs <= 2 * kNumCUs ? 4 : 2;
+    const size_t parts = (size_t)d->Hkv * s.num_splits;
+    const size_t padded = (rows + kRowBlock - 1) / kRowBlock * kRowBlock; // whole row blocks
+    pl.acc_bytes = align_up(parts * (f32 ? rows * d->d * sizeof(float) : padded * d->d * sizeof(uint16_t)));
+    pl.ml_bytes = align_up(parts * rows * (f32 ? 2 : 4) * sizeof(float));
     return pl;
 }
 
@@ -97,8 +120,13 @@ SharedParams shared_params(const AttnParams& base, const Cut& c, const SharedPla
     p.shared_len = shared_len;
     p.shared_table = prefix.paged ? prefix.block_table : nullptr;
     p.sh_rows = d->B * d->T * (d->Hq / d->Hkv);
+    p.sh_blocks = (p.sh_rows + kRowBlock - 1) / kRowBlock;
     p.sh_splits = pl.shared.num_splits;
     p.sh_keys_per_split = pl.shared.keys_per_split;
+    p.sh_shares = pl.shares;
+    p.sh_groups = pl.shared.row_groups;
+    p.sh_units = d->Hkv * pl.shared.row_groups;
+    p.sh_by_rows = fast_div_by(pl.shared.rows_per_group);
     p.max_shared = prefix.max_prefix_len;
     while (prefix.paged && (1 << p.sh_block_shift) < prefix.block_size) ++p.sh_block_shift;
     p.sh_num_blocks = prefix.num_blocks;
@@ -135,8 +163,8 @@ int32_t vs_shared_prefix_attention(const vs_attn_desc* desc, const vs_prefix_des
                                              shared_len, workspace);
     const SharedParams second = shared_params(attention_params(desc, 1, q, k_cache, v_cache, prefix_len, tree_parent, tree_mask, out, status), pl.own, pl, desc, x,
                                               shared_len, workspace);
-    hipError_t e = f32 ? launch_attention_shared_f32(first, kRowsShared, s) : launch_attention_shared_rows(first, kRowsShared, s);
-    if (e == hipSuccess) e = f32 ? launch_attention_shared_f32(second, kRowsOwn, s) : launch_attention_shared_rows(second, kRowsOwn, s);
+    hipError_t e = f32 ? launch_attention_shared_f32(first, kRowsShared, s) : pl.waves ? launch_attention_shared_pipe(first, kRowsShared, pl.waves, s) : launch_attention_shared_rows(first, kRowsShared, 8, s);
+    if (e == hipSuccess) e = f32 ? launch_attention_shared_f32(second, kRowsOwn, s) : pl.own_pipe ? launch_attention_shared_pipe(second, kRowsOwn, pl.own_waves, s) : launch_attention_shared_rows(second, kRowsOwn, pl.own_waves, s);
     return e == hipSuccess ? VS_OK : VS_ERR_HIP;
 }
 

@@ -75,6 +75,11 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const st
     const int kb = lane >> 4, cg = (lane >> 2) & 3, j = lane & 3;
 
     // the row groups of a unit run on one XCD and share its L2 (one split)
+    if constexpr (MODE == kRowsOwn)
+        if (blockIdx.x >= round_up8(p.total_wgs)) {
+            report_shared(p, (int)round_up8(p.total_wgs));
+            return;
+        }
     const WorkItem at = work_item(p);
     if (at.none) return;
     const int rg = at.rg, kvh = at.kvh, b = at.b;
@@ -165,9 +170,8 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const st
         tree_code = load_tree(p.parent + (int64_t)b * p.T, p.T, sp, &sflag);
     }
     const bool s_ok = prefix_ok(p, S);
-    if (kvh == 0 && rg == 0) report_status(p, b, tree_code, s_ok, S, &sflag);
-    if constexpr (MODE == kRowsOwn)
-        if (kvh == 0 && rg == 0) report_shared(p, b, &sflag);
+    if constexpr (MODE != kRowsOwn)
+        if (kvh == 0 && rg == 0) report_status(p, b, tree_code, s_ok, S, &sflag);
     if (tree_code != VS_STATUS_OK || !s_ok) return;
     if (!given && p.tree_keys != 0) {
 #pragma unroll
@@ -380,7 +384,7 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const st
             if (c == 0) *(f32x2*)(p.sh_ml + to * 2) = row_ml[row];
             return;
         } else if constexpr (MODE == kRowsOwn) {
-            const int parts = shared_parts(p);
+            const int parts = shared_parts(p, p.shared_len[0], kvh, b * p.rows + r);
             float m = row_ml[row][0], l = row_ml[row][1];
             for (int s = 0; s < parts; ++s) {
                 const int64_t from = shared_row(p, kvh, s, b * p.rows + r);
@@ -410,7 +414,7 @@ hipError_t launch_f32(const AttnParams& p, hipStream_t s) {
 
 template <int D, int SETS, int MODE>
 void launch_f32_shared(const SharedParams& p, hipStream_t s) {
-    const dim3 grid((p.total_wgs + 7) / 8 * 8), block(kF32Waves * kWave);
+    const dim3 grid(round_up8(p.total_wgs) + (MODE == kRowsOwn && p.status ? (p.B + kF32Waves - 1) / kF32Waves : 0)), block(kF32Waves * kWave);
     if (p.paged) hipLaunchKernelGGL((attn_f32_kernel<D, SETS, true, MODE>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((attn_f32_kernel<D, SETS, false, MODE>), grid, block, 0, s, p);
 }

@@ -28,16 +28,20 @@
 // fragments read three or four slots ahead: nothing.)
 #include <type_traits>
 
-#include "attn_mfma_common.h"
+#include "attn_shared.h"
 
 namespace vs {
 
 namespace {
 
 // Waves of a SIMD that have registers at the same time: two, and three (workgroups of four waves on a CU) with 64 channels.
-template <int D, int RPW, int NW, bool PAGED, bool BAL, bool ONCE>
-__global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma_pipe_kernel(const AttnParams p) {
+// MODE (attn_shared.h): kRowsShared, all sequences' rows against the keys that they share: equal shares of all row groups' keys, whose pieces
+// leave as partial results in fp32; kRowsOwn, a sequence's rows against its own keys, joined with those.
+template <int D, int RPW, int NW, bool PAGED, bool BAL, bool ONCE, int MODE = kRowsWhole>
+__global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma_pipe_kernel(const std::conditional_t<MODE == kRowsWhole, AttnParams, SharedParams> p) {
     request_args(p);
+    constexpr bool SHARED = MODE == kRowsShared, OWN = MODE == kRowsOwn;
+    constexpr bool PIECES = BAL || SHARED; // a workgroup has several pieces of work, and knows the sequences' lengths
     constexpr int KS = D / 16;                 // k-steps of the S^T product
     constexpr int DB = D / 32;                 // 32-channel blocks of the output
     constexpr int SUB = kTileKeys * D;         // elements per 32-key tile of K (or V)
@@ -105,7 +109,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     // needs. Four waves of 128 channels had 41 of them in scratch memory, and the wait for a spilled value in the
     // loop waits for all tile copies in flight: 20 x 60 nodes, 32 / 32 heads, 250 .. 2000 keys 131 us, so 117
     // (8 of 1024 .. 8191 keys 159 / 147, paged 163 / 154; eight waves: no spills either, 1 %).
-    if (BAL) asm volatile("" : "+v"(tid));
+    if (PIECES) asm volatile("" : "+v"(tid));
     const int lane = tid & 63, half = lane >> 5, col = lane & 31;
     // The prefix length is requested first and needed last: the first tiles and the queries are requested before it arrives. DIRECT: it and the
     // first block ids come through LDS like the tiles and are waited for by counting loads, since the compiler, which does not know of loads
@@ -113,8 +117,8 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     // (Before, the wave waited for the length, and paged for the queries, before it asked for the tiles: us per layer, 28 / 4 heads, before /
     // so: 6 x 60 nodes, 2044 .. 4089 keys paged 33.2 / 32.3; 6 x 23, 903 .. 1806 keys 17.9 / 17.4; longer launches 0 - 1 %.)
     int32_t S = S_known;
-    if constexpr (DIRECT && !BAL) load_to_lds4((uint32_t)(uintptr_t)(lds_void*)&sLen[wave][0], p.prefix_len + b, 0u);
-    else if constexpr (!BAL) S = p.prefix_len[b];
+    if constexpr (DIRECT && !PIECES) load_to_lds4((uint32_t)(uintptr_t)(lds_void*)&sLen[wave][0], p.prefix_len + b, 0u);
+    else if constexpr (!PIECES) S = p.prefix_len[b];
 
     // ---- tile copies. One load instruction of a wave fetches 1 KB of consecutive memory:
     // RPI whole rows (tokens) of D channels, lane q -> row q / LPR, 16-byte chunk q % LPR, so
@@ -249,7 +253,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
         }
         bt_set(bt_first);
     }
-    constexpr bool EARLY = DIRECT || !(BAL && PAGED); // registers: 4 waves of 128 channels 188 us, so 171 (8 x 60 nodes, 32 / 32 heads, 1024 .. 8191 keys)
+    constexpr bool EARLY = DIRECT || !(PIECES && PAGED); // registers: 4 waves of 128 channels 188 us, so 171 (8 x 60 nodes, 32 / 32 heads, 1024 .. 8191 keys)
     // this lane's 16 bytes of the block at a uniform address: a scalar address plus lane_off. (The second statement keeps the
     // lane's part in one register: extended to 64 bits in front of the loop it takes two and an addition per copy.)
     auto load_at = [&](const void* block) __attribute__((always_inline)) {
@@ -265,7 +269,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     // table's). Values of rows that turn out to lie past the sequence's last key become zeros in LDS (DIRECT: zero_tail) or on their way there from register set 1: whatever the cache holds there, NaN included,
     // must not meet a zero probability.
     if constexpr (EARLY) {
-        const int kend = early_end(BAL ? S_known + p.tree_keys : most_keys(p), k0, klen);
+        const int kend = early_end(PIECES ? S_known + p.tree_keys : most_keys(p), k0, klen);
         if constexpr (DIRECT) rows_up_to(kend);
         auto load_tile_early = [&](auto is_v, int t, u32x4(&r)[BPW]) __attribute__((always_inline)) {
             const uint16_t* gbase = decltype(is_v)::value ? vbase : kbase;
@@ -306,22 +310,23 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     } else {
         tree_code = load_tree(p.parent + (int64_t)b * p.T, p.T, sp, &sflag);
     }
-    if constexpr (DIRECT && !BAL) {
+    if constexpr (DIRECT && !PIECES) {
         // loads behind it: those above, the fewest of any wave
         constexpr int TILES_K = Q_K < NSLOT - 1 ? Q_K : NSLOT - 1;
         wait_loads<(PAGED ? 2 : 0) + KS + (HALVES ? (TILES_K < Q_V ? TILES_K : Q_V) : TILES_K + Q_V)>();
         S = __builtin_amdgcn_readfirstlane(sLen[wave][0]);
     }
     const bool s_ok = prefix_ok(p, S);
-    if (reports) report_status(p, b, tree_code, s_ok, S, &sflag);
+    if constexpr (!OWN)
+        if (reports) report_status(p, b, tree_code, s_ok, S, &sflag);
     const int nk = S + p.tree_keys;
     if (tree_code != VS_STATUS_OK || !s_ok || k0 >= nk) { // uniform
         wait_loads<0>(); // tiles (DIRECT) and queries on their way to LDS
-        if (BAL) __syncthreads(); // other pieces follow, or merges that take the rings' place
+        if (PIECES) __syncthreads(); // other pieces follow, or merges that take the rings' place
         return;
     }
-    if (!BAL && p.gates && nk <= klen) whole = true; // a sequence of one split has nothing to merge
-    const bool merge = !BAL && p.gates && !whole;
+    if (!PIECES && p.gates && nk <= klen) whole = true; // a sequence of one split has nothing to merge
+    const bool merge = !PIECES && p.gates && !whole;
     uint64_t* const gate = merge ? p.gates + kGateWords * (((int64_t)b * p.Hkv + kvh) * p.row_groups + rg) : nullptr;
     if (merge && tid == 0) merge_open(gate, gate_load(gate));
     const int k1 = min(nk, k0 + klen);
@@ -706,7 +711,9 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     }
     // tiles that end at or before min(S, k1) hold prefix keys only
     const int n_plain = max(0, min(S, k1) - k0) / kTileKeys;
-    const int fast_end = min(n_plain, n - 1) & ~1; // fast iterations need tiles ta + 1 (plain) and ta + 2 (present)
+    // fast iterations need tiles ta + 1 (plain) and ta + 2 (present; SHARED: or not - of a tile behind the last one only scores are made, which nobody
+    // looks at, from whatever its slot holds)
+    const int fast_end = SHARED && n_plain == n ? n & ~1 : min(n_plain, n - 1) & ~1;
     // what the first fast step takes for V(-1), with probabilities of zero
     if (fast_end > (DIRECT ? 0 : 2))
         for (int i = tid * 8; i < SUB; i += NW * 64 * 8) *(u32x4*)&sV[NSLOT - 1][i] = u32x4{0u, 0u, 0u, 0u};
@@ -858,6 +865,51 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
 #pragma unroll
     for (int rb = 0; rb < RPW; ++rb) {
         const float l = half_sum(lsum[rb] + lsum2[rb]);
+        if constexpr (SHARED) {
+            const int r_local = row_base + rb * kRowBlock + col;
+            if (r_local >= p.rows) continue;
+            char* const to = shared_means<D>(p, kvh, slot, r_local, half);
+            const float inv = 1.f / l;
+            u32x4 head = {__float_as_uint(m2[rb]), __float_as_uint(l), 0u, 0u};
+#pragma unroll
+            for (int pc = 0; pc < 2 * DB; ++pc) {
+                float mean[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) mean[e] = acc[rb][pc >> 1][8 * (pc & 1) + e] * inv;
+                uint32_t exponent;
+                *(u32x4*)(to + pc * 1024) = pack_means(mean, exponent);
+                head[2 + pc / 4] |= exponent << (8 * (pc & 3));
+            }
+            if (half == 0) *(u32x4*)shared_head(p, kvh, slot, r_local) = head;
+            continue;
+        }
+        if constexpr (OWN) {
+            // the row's own part joined with those against the shared keys
+            const int r_local = row_base + rb * kRowBlock + col;
+            const SharedRow row = shared_at<D>(p, p.shared_len[0], kvh, b * p.rows + min(r_local, p.rows - 1), half);
+            uint16_t* o = (uint16_t*)p.out + row_offset(p, b, kvh, min(r_local, p.rows - 1), row_node(p, min(r_local, p.rows - 1))) + 4 * half;
+            constexpr int G = 2 * DB; // all pieces
+#pragma unroll
+            for (int pc = 0; pc < 2 * DB; pc += G) {
+                JoinParts<D == 128 ? 3 : 4, G> parts;
+                load_parts(row, 0, pc, parts);
+                float x[G][8];
+#pragma unroll
+                for (int i = 0; i < G; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[i][e] = acc[rb][(pc + i) >> 1][8 * ((pc + i) & 1) + e];
+                float sum = l;
+                join_row(row, pc, parts, m2[rb], sum, x);
+                if (r_local < p.rows) {
+                    const float inv = 1.f / sum;
+#pragma unroll
+                    for (int i = 0; i < G; ++i)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) *(u32x2*)(o + (pc + i) * 16 + 8 * h) = pack_partial(x[i][4 * h], x[i][4 * h + 1], x[i][4 * h + 2], x[i][4 * h + 3], inv);
+                }
+            }
+            continue;
+        }
         if (whole) {
             // Lines pay for eight waves of 128 channels: us per call, 8-byte pieces / lines, 60 nodes, 28 / 4 heads, 64 x 400 keys 53.4 / 48.7,
             // 28 x 1696 59.9 / 58.6. With four waves or 64 channels the trip through LDS costs more: 12 x 35 nodes, 32 / 32
@@ -907,7 +959,29 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     }
     }; // run_piece
 
-    if constexpr (!BAL) {
+    if constexpr (SHARED) {
+        // workgroup -> share; consecutive shares, which read neighbouring keys of one KV head, on one XCD
+        const int w = (int)((blockIdx.x & 7) * (uint32_t)((p.sh_shares + 7) >> 3) + (blockIdx.x >> 3));
+        const int32_t len = p.shared_len[0];
+        if (w >= p.sh_shares || !shared_ok(p, len) || len == 0) return;
+        const uint32_t steps = (uint32_t)(len + kIterKeys - 1) / kIterKeys;
+        const uint64_t total = (uint64_t)p.sh_units * steps;
+        const uint64_t hi = share_begin(p, total, w + 1);
+        for (uint64_t lo = share_begin(p, total, w); lo < hi;) {
+            const uint32_t u = __builtin_amdgcn_readfirstlane((uint32_t)(lo / steps)), t0 = __builtin_amdgcn_readfirstlane((uint32_t)(lo - (uint64_t)u * steps));
+            const uint32_t t1 = __builtin_amdgcn_readfirstlane((uint32_t)min((uint64_t)steps, t0 + (hi - lo)));
+            uint32_t rg;
+            const int kvh = (int)fast_div(u, p.by_groups, rg);
+            run_piece(0, kvh, (int)rg, (int)t0 * kIterKeys, (int)(t1 - t0) * kIterKeys, w - first_share(p, total, steps, u), false, len);
+            lo += t1 - t0;
+            if (lo < hi) __syncthreads(); // the last reads of the tile rings
+        }
+    } else if constexpr (!BAL) {
+        if constexpr (OWN)
+            if (blockIdx.x >= round_up8(p.total_wgs)) {
+                report_shared(p, (int)round_up8(p.total_wgs));
+                return;
+            }
         int b, kvh, rg, split = 0;
         if (p.by_length) {
             // More workgroups than run at once, one per (sequence, KV head, row group): the longest
@@ -1074,6 +1148,27 @@ hipError_t launch_pipe(const AttnParams& p, hipStream_t s) {
 }
 
 } // namespace
+
+namespace {
+template <int D, int NW, int MODE>
+hipError_t launch_pipe_shared(const SharedParams& p, hipStream_t s) {
+    const dim3 grid(MODE == kRowsShared ? round_up8(p.sh_shares) : round_up8(p.total_wgs) + (p.status ? (p.B + NW - 1) / NW : 0)), block(NW * kWave);
+    if (p.paged) hipLaunchKernelGGL((attn_mfma_pipe_kernel<D, 1, NW, true, false, false, MODE>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((attn_mfma_pipe_kernel<D, 1, NW, false, false, false, MODE>), grid, block, 0, s, p);
+    return hipGetLastError();
+}
+template <int MODE>
+hipError_t launch_pipe_shared(const SharedParams& p, int waves, hipStream_t s) {
+    if (p.d == 128) return waves == 8 ? launch_pipe_shared<128, 8, MODE>(p, s) : launch_pipe_shared<128, 4, MODE>(p, s);
+    return waves == 8 ? launch_pipe_shared<64, 8, MODE>(p, s) : launch_pipe_shared<64, 4, MODE>(p, s);
+}
+} // namespace
+
+hipError_t launch_attention_shared_pipe(const SharedParams& p, RowsMode mode, int waves, hipStream_t s) {
+    if ((waves != 4 && waves != 8) || p.rows_per_group != waves * kRowBlock || (p.d != 128 && p.d != 64)) return hipErrorInvalidValue;
+    if (mode == kRowsShared ? p.sh_shares < 1 : p.num_splits != 1 || p.row_groups * p.rows_per_group < p.rows) return hipErrorInvalidValue;
+    return mode == kRowsShared ? launch_pipe_shared<kRowsShared>(p, waves, s) : launch_pipe_shared<kRowsOwn>(p, waves, s);
+}
 
 // One row block per wave; four waves (two workgroups per CU) or eight.
 bool attention_pipe_supported(int rpw, int waves) { return rpw == 1 && (waves == 4 || waves == 8); }

@@ -73,6 +73,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
         b = sequence_by_rank(p, (int)fast_div(blockIdx.x, p.by_heads, head), lane);
         kvh = (int)head;
     } else {
+        if constexpr (MODE == kRowsOwn)
+            if (blockIdx.x >= round_up8(p.total_wgs)) {
+                report_shared(p, (int)round_up8(p.total_wgs));
+                return;
+            }
         const WorkItem at = work_item(p);
         if (at.none) return;
         b = at.b;
@@ -164,6 +169,21 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
     uint64_t* const gate = MODE == kRowsWhole && p.gates ? p.gates + kGateWords * ((int64_t)unit * p.row_groups + rg) : nullptr;
     uint64_t seen = 0;
     if (MODE == kRowsWhole && p.gates && wave == 0) seen = gate_load(gate);
+    // kRowsOwn: this wave's pieces of the first parts against the shared keys
+    constexpr int PPW = NP / NW > 0 ? NP / NW : 1;
+    constexpr int EARLY = MODE == kRowsOwn ? (PPW == 1 ? 8 : 4) : 1;
+    JoinParts<EARLY, PPW> parts; // (two row blocks have no registers for them yet)
+    SharedRow joined[MODE == kRowsOwn ? RB : 1];
+    int32_t shared = 0;
+    const int my_piece = min(wave, NP / PPW - 1) * PPW;
+    if constexpr (MODE == kRowsOwn) {
+        shared = p.shared_len[0];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            joined[rb] = shared_at<D>(p, shared, kvh, b * p.rows + min(row0 + rb * kRowBlock + col, p.rows - 1), half);
+        }
+        if constexpr (RB == 1) load_parts(joined[0], 0, my_piece, parts);
+    }
     if (first < kend) { // uniform per wave
         issue(std::false_type{}, sK, first, kend - 1);
         issue(std::true_type{}, sV, first, kend - 1);
@@ -181,9 +201,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
         }
     }
     const bool s_ok = prefix_ok(p, S);
-    if (kvh == 0 && split == 0 && rg == 0) report_status<PAGED>(p, b, tree_code, s_ok, S, &sflag);
-    if constexpr (MODE == kRowsOwn)
-        if (kvh == 0 && rg == 0) report_shared(p, b, &sflag);
+    if constexpr (MODE != kRowsOwn)
+        if (kvh == 0 && split == 0 && rg == 0) report_status<PAGED>(p, b, tree_code, s_ok, S, &sflag);
     if (tree_code != VS_STATUS_OK || !s_ok) return;
     const int nk = S + p.tree_keys;
     if (k0 >= nk) return;
@@ -329,13 +348,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
         }
     }
     wait_loads<0>(); // (a wave without a live tile may have requested one)
-    int parts = 0;
-    if constexpr (MODE == kRowsOwn) parts = shared_parts(p);
 
     // ---- merge the waves' results through LDS (log-sum-exp) and write the rows. The accumulators are NP pieces of eight
     // registers (piece = channel block * 2 + half of its registers, the 16-byte unit of the partial-result layout):
     // wave w owns pieces w * PPW .., takes the other waves' versions of them and merges in ascending order.
-    constexpr int PPW = NP / NW > 0 ? NP / NW : 1;
     // A wave hands its first row block over in the place of its own tiles, as soon as it is done with them: the last one then
     // writes alone, and one barrier less (us: 3 x 2 nodes, 8 / 2 heads, 330 keys 6.9, so 6.5; 18 x 1, 28 / 4 heads, 1600 keys 16.5 / 16.1; 4 x 60,
     // 32 / 32 heads, ~3100 keys 47.9 / 47.5).
@@ -392,29 +408,26 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
             float inv = l > 0.f ? 1.f / l : 0.f; // no visible key in this split (partials only): zeros, weight 0
             if constexpr (MODE != kRowsWhole) {
                 const int row = row0 + rb * kRowBlock + col;
-                f32x4 o[2 * PPW]; // channels at(i) .. + 3 of the lane's row
-                auto at = [&](int i) __attribute__((always_inline)) { return (wave * PPW + (i >> 1)) * 16 + (i & 1) * 8 + 4 * half; };
-#pragma unroll
-                for (int i = 0; i < PPW; ++i) {
-                    o[2 * i] = f32x4{r[i][0], r[i][1], r[i][2], r[i][3]};
-                    o[2 * i + 1] = f32x4{r[i][4], r[i][5], r[i][6], r[i][7]};
-                }
                 if constexpr (MODE == kRowsShared) {
-                    if (row >= p.rows) continue;
-                    const int64_t to = shared_row(p, kvh, split, row);
+                    if (row >= p.rows) continue; // (both halves of a row)
+                    char* const to = shared_means<D>(p, kvh, split, row, half);
+                    char* const head = shared_head(p, kvh, split, row);
 #pragma unroll
-                    for (int i = 0; i < 2 * PPW; ++i) *(f32x4*)(p.sh_acc + to * D + at(i)) = o[i];
-                    if (wave == 0 && half == 0) *(f32x2*)(p.sh_ml + to * 2) = f32x2{M, l};
+                    for (int i = 0; i < PPW; ++i) {
+                        float mean[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) mean[e] = r[i][e] * inv;
+                        uint32_t exponent;
+                        *(u32x4*)(to + (my_piece + i) * 1024) = pack_means(mean, exponent);
+                        if (half == 0) head[8 + my_piece + i] = (char)exponent;
+                    }
+                    if (wave == 0 && half == 0) *(f32x2*)head = f32x2{M, l};
                     continue;
                 } else {
-                    inv = join_shared<D>(p, kvh, b * p.rows + min(row, p.rows - 1), parts, M, l, o, at);
-#pragma unroll
-                    for (int i = 0; i < PPW; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            r[i][e] = o[2 * i][e];
-                            r[i][4 + e] = o[2 * i + 1][e];
-                        }
+                    float sum = l;
+                    if constexpr (RB > 1) load_parts(joined[rb], 0, my_piece, parts);
+                    join_row(joined[rb], my_piece, parts, M, sum, r);
+                    inv = 1.f / sum;
                 }
             }
 #pragma unroll
@@ -463,26 +476,29 @@ hipError_t launch_rows(const AttnParams& p, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <int D, int RB, int MODE>
+template <int D, int NW, int RB, int MODE>
 hipError_t launch_shared(const SharedParams& p, hipStream_t s) {
-    const dim3 grid(((p.total_wgs + 7) / 8) * 8), block(8 * kWave);
-    if (p.paged) hipLaunchKernelGGL((attn_mfma_rows_kernel<D, 8, RB, true, false, false, MODE>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((attn_mfma_rows_kernel<D, 8, RB, false, false, false, MODE>), grid, block, 0, s, p);
+    const dim3 grid(round_up8(p.total_wgs) + (MODE == kRowsOwn && p.status ? (p.B + NW - 1) / NW : 0)), block(NW * kWave);
+    if (p.paged) hipLaunchKernelGGL((attn_mfma_rows_kernel<D, NW, RB, true, false, false, MODE>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((attn_mfma_rows_kernel<D, NW, RB, false, false, false, MODE>), grid, block, 0, s, p);
     return hipGetLastError();
 }
-template <int MODE>
-hipError_t launch_shared(const SharedParams& p, int blocks, hipStream_t s) {
-    if (p.d == 128) return blocks == 2 ? launch_shared<128, 2, MODE>(p, s) : launch_shared<128, 1, MODE>(p, s);
-    return launch_shared<64, 1, MODE>(p, s);
+template <int D>
+hipError_t launch_shared_own(const SharedParams& p, int waves, hipStream_t s) {
+    return waves == 8 ? launch_shared<D, 8, 1, kRowsOwn>(p, s) : waves == 4 ? launch_shared<D, 4, 1, kRowsOwn>(p, s) : launch_shared<D, 2, 1, kRowsOwn>(p, s);
 }
 
 } // namespace
 
-hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, hipStream_t s) {
+hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, int waves, hipStream_t s) {
     const int blocks = p.rows_per_group / kRowBlock;
     if (p.row_groups * p.rows_per_group < p.rows || (p.d != 64 && p.d != 128) || blocks < 1 || blocks > (p.d == 128 ? 2 : 1)) return hipErrorInvalidValue;
     if (p.keys_per_split % kIterKeys || (mode == kRowsOwn && p.num_splits != 1)) return hipErrorInvalidValue;
-    return mode == kRowsShared ? launch_shared<kRowsShared>(p, blocks, s) : launch_shared<kRowsOwn>(p, blocks, s);
+    if (mode == kRowsOwn && blocks == 1) return p.d == 128 ? launch_shared_own<128>(p, waves, s) : launch_shared_own<64>(p, waves, s);
+    if (waves != 8) return hipErrorInvalidValue;
+    if (mode == kRowsOwn) return launch_shared<128, 8, 2, kRowsOwn>(p, s);
+    if (p.d == 64) return launch_shared<64, 8, 1, kRowsShared>(p, s);
+    return blocks == 2 ? launch_shared<128, 8, 2, kRowsShared>(p, s) : launch_shared<128, 8, 1, kRowsShared>(p, s);
 }
 
 // One row block and four or eight waves; with 128 channels also two row blocks and eight waves.

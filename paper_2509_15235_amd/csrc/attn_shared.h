@@ -1,62 +1,169 @@
 // Partial results of rows against the keys that all sequences share, and how a sequence's own part is joined with them.
 //
-// A row's softmax over shared and own keys is taken in parts: part i has a reference m_i (log2 domain), the sum l_i of its weights 2^(s - m_i) and
-// the sum o_i of weights times values; with M the largest reference the row is sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.
-// The parts of the shared keys are written and read in fp32: a row is then rounded once, as if all its keys had been in one place.
+// A row's softmax over shared and own keys is taken in parts: part i has a reference m_i (log2 domain), the sum l_i of its weights 2^(s - m_i) and the
+// weighted mean o_i of its values; with M the largest reference the row is sum_i 2^(m_i - M) l_i o_i / sum_i 2^(m_i - M) l_i.
+// References and sums are fp32. fp32 storage keeps fp32 means too. For bf16 storage they are what a call writes and reads most of beside K and V (16 x 60
+// nodes of 28 / 4 heads, three parts or so of every row: 47 MB in fp32), so they are kept as fp16 with a power of two of its own for every 16 channels
+// of a row: 11 bits, whatever the values' size, of which 2^29 lie between the largest and the first that loses bits. That rounding, 2^-12, is an eighth of
+// the result's own, 2^-9 at most; a bf16 mean would double what two roundings to bf16 - the weights', the result's - are off by.
 #pragma once
 
 #include "attn_mfma_common.h"
 
 namespace vs {
 
-// How many parts there are of the shared keys: none where their number is not one (which is reported), or zero.
 __device__ __forceinline__ bool shared_ok(const SharedParams& p, int32_t len) { return len >= 0 && len <= p.max_shared && len <= p.sh_slots; }
-__device__ __forceinline__ int shared_parts(const SharedParams& p) {
-    const int32_t len = p.shared_len[0];
-    return shared_ok(p, len) ? (len + p.sh_keys_per_split - 1) / p.sh_keys_per_split : 0;
+
+// ---- Equal shares: all units - (KV head, row group), a KV head's next to each other - have the same `steps` of 64 keys, laid end to end; share w
+// takes the steps from w * total / shares on. A unit's parts are the pieces of consecutive shares.
+__device__ __forceinline__ uint64_t share_begin(const SharedParams& p, uint64_t total, int w) { return (uint64_t)w * total / (uint32_t)p.sh_shares; }
+// the share that step x lies in: the largest w with w * total / shares <= x
+__device__ __forceinline__ int share_of(const SharedParams& p, uint64_t total, uint64_t x) { return (int)(((x + 1) * (uint32_t)p.sh_shares - 1) / total); }
+__device__ __forceinline__ int first_share(const SharedParams& p, uint64_t total, uint32_t steps, uint32_t unit) { return share_of(p, total, (uint64_t)unit * steps); }
+
+// How many parts there are of a row against the shared keys (none where their number is not one, which is reported, or zero).
+__device__ __forceinline__ int shared_parts(const SharedParams& p, int32_t len, int kvh, int row) {
+    if (!shared_ok(p, len) || len == 0) return 0;
+    if (p.sh_shares == 0) return (len + p.sh_keys_per_split - 1) / p.sh_keys_per_split;
+    const uint32_t steps = (uint32_t)(len + kIterKeys - 1) / kIterKeys;
+    const uint64_t total = (uint64_t)p.sh_units * steps;
+    uint32_t rest;
+    const uint32_t unit = (uint32_t)kvh * p.sh_groups + fast_div((uint32_t)row, p.sh_by_rows, rest);
+    return share_of(p, total, (uint64_t)(unit + 1) * steps - 1) - first_share(p, total, steps, unit) + 1;
 }
-// first element of (KV head, split, row)'s pair
-__device__ __forceinline__ int64_t shared_row(const SharedParams& p, int kvh, int split, int row) {
-    return ((int64_t)kvh * p.sh_splits + split) * p.sh_rows + row;
+// Number of (KV head, part, row). fp32 storage: its pair (m, l) and its d sums of weights times values lie there.
+__device__ __forceinline__ int64_t shared_row(const SharedParams& p, int kvh, int part, int row) {
+    return ((int64_t)kvh * p.sh_splits + part) * p.sh_rows + row;
 }
-// Joins what a lane holds of a row - N groups of four channels, group i at channel at(i) - with the parts of the shared keys: `row` counts the rows of
-// all sequences. On return o is to be multiplied by the returned factor.
-template <int D, int N, typename At>
-__device__ __forceinline__ float join_shared(const SharedParams& p, int kvh, int row, int parts, float m, float l, f32x4 (&o)[N], At at) {
-    for (int s = 0; s < parts; ++s) {
-        const int64_t r = shared_row(p, kvh, s, row);
-        const f32x2 ml = *(const f32x2*)(p.sh_ml + r * 2);
-        f32x4 x[N];
+// bf16 storage: sixteen bytes of m, l and the exponents of the row's pieces of 16 channels, and the means as the accumulators hold them, so that whoever
+// writes or reads them moves runs of memory: the sixteen bytes of channels 16 pc + 4 half .. + 3 and 8 behind those of row r are number
+// ((block of r) * D / 16 + pc) * 64 + 32 half + r % 32 of the part.
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+template <int D>
+__device__ __forceinline__ char* shared_means(const SharedParams& p, int kvh, int part, int row, int half) {
+    const int64_t block = ((int64_t)kvh * p.sh_splits + part) * p.sh_blocks + (row >> 5);
+    return (char*)p.sh_acc + (block * (D / 16) * 64 + half * 32 + (row & 31)) * 16;
+}
+__device__ __forceinline__ char* shared_head(const SharedParams& p, int kvh, int part, int row) { return (char*)p.sh_ml + shared_row(p, kvh, part, row) * 16; }
+// Eight values (both halves' are one piece) as fp16; `exponent`: what gives them back, plus 128. The largest becomes 2^14 .. 2^15.
+__device__ __forceinline__ u32x4 pack_means(const float (&x)[8], uint32_t& exponent) {
+    float top = fabsf(x[0]);
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = *(const f32x4*)(p.sh_acc + r * D + at(i));
-        const float M = fmaxf(m, ml[0]), f = __builtin_amdgcn_exp2f(m - M), g = __builtin_amdgcn_exp2f(ml[0] - M);
-        l = l * f + ml[1] * g;
+    for (int e = 1; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+    top = half_max(top);
+    const int k = min(141 - (int)(__float_as_uint(top) >> 23), 100);
+    exponent = (uint32_t)(128 - k);
+    u32x4 w;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[i][e] = o[i][e] * f + x[i][e] * g;
-        m = M;
+    for (int e = 0; e < 4; ++e) {
+        const f32x2 v = {__builtin_amdgcn_ldexpf(x[2 * e], k), __builtin_amdgcn_ldexpf(x[2 * e + 1], k)};
+        w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
     }
-    return 1.f / l;
+    return w;
 }
-// The workgroup that reports a sequence's status (all of its threads) also looks at what all sequences share. `own`: the code so far, which
-// comes first, known to thread 0.
-__device__ __forceinline__ void report_shared(const SharedParams& p, int b, int32_t* sflag) {
-    if (!p.status) return;
-    const int32_t len = p.shared_len[0];
-    const bool ok = shared_ok(p, len);
-    __syncthreads(); // sflag has been read
-    if (threadIdx.x == 0) *sflag = 0;
-    __syncthreads();
-    if (ok && p.shared_table)
-        for (int i = threadIdx.x; i < (len + (1 << p.sh_block_shift) - 1) >> p.sh_block_shift; i += blockDim.x)
-            if ((uint32_t)p.shared_table[i] >= (uint32_t)p.sh_num_blocks) atomicOr(sflag, 8);
-    __syncthreads();
-    if (threadIdx.x == 0 && p.status[b] == VS_STATUS_OK) { // this thread's own store
-        if (!ok) p.status[b] = VS_STATUS_BAD_PREFIX;
-        else if (*sflag & 8) p.status[b] = VS_STATUS_BAD_BLOCK;
+
+// ---- Joining a row's own part with its parts against the shared keys. Those were written by the launch before, so the first of
+// them are asked for when a workgroup begins, and are there when its own keys are done.
+struct SharedRow { // a lane's row
+    int parts;
+    const char* head;   // of its first part
+    const char* means;  // its sixteen bytes of piece 0 in the first part
+    int64_t head_step, step; // bytes from a part to the next
+};
+template <int D>
+__device__ __forceinline__ SharedRow shared_at(const SharedParams& p, int32_t len, int kvh, int row, int half) {
+    return {shared_parts(p, len, kvh, row), shared_head(p, kvh, 0, row), shared_means<D>(p, kvh, 0, row, half), (int64_t)p.sh_rows * 16, (int64_t)p.sh_blocks * (kRowBlock * D * 2)};
+}
+constexpr int kJoinHeads = 8; // references in flight
+// N parts from s0 on, G pieces from pc on. Past the last part the last one again.
+template <int N, int G>
+struct JoinParts {
+    u32x4 head[N];
+    u32x4 x[N][G];
+};
+template <int N, int G>
+__device__ __forceinline__ void load_parts(const SharedRow& r, int s0, int pc, JoinParts<N, G>& j) {
+    const int last = max(r.parts - 1, 0); // (no parts: the first place, which is there, is read and not used)
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+        const int64_t part = min(s0 + s, last);
+        j.head[s] = *(const u32x4*)(r.head + part * r.head_step);
+#pragma unroll
+        for (int i = 0; i < G; ++i) j.x[s][i] = *(const u32x4*)(r.means + part * r.step + (pc + i) * 1024);
     }
-    __syncthreads();
+}
+// The common reference of a row's own part (reference m) and all others.
+template <int N, int G>
+__device__ __forceinline__ float join_reference(const SharedRow& r, const JoinParts<N, G>& first, float m) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) m = s < r.parts ? fmaxf(m, __uint_as_float(first.head[s][0])) : m;
+    for (int s0 = N; s0 < r.parts; s0 += kJoinHeads) {
+        float x[kJoinHeads];
+#pragma unroll
+        for (int s = 0; s < kJoinHeads; ++s) x[s] = *(const float*)(r.head + (int64_t)min(s0 + s, r.parts - 1) * r.head_step);
+#pragma unroll
+        for (int s = 0; s < kJoinHeads; ++s) m = fmaxf(m, x[s]);
+    }
+    return m;
+}
+// Adds parts to sums that are relative to the reference M, and to the sum of weights l.
+template <int N, int G>
+__device__ __forceinline__ void join_parts(const SharedRow& r, int s0, int pc, const JoinParts<N, G>& j, float M, float& l, float (&o)[G][8]) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) {
+        const bool there = s0 + s < r.parts;
+        const float w = there ? __builtin_amdgcn_exp2f(__uint_as_float(j.head[s][0]) - M) * __uint_as_float(j.head[s][1]) : 0.f;
+        l += w;
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            const uint32_t word = pc + i < 4 ? j.head[s][2] : j.head[s][3];
+            const float f = __builtin_amdgcn_ldexpf(w, (int)((word >> (8 * ((pc + i) & 3))) & 0xff) - 128);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t two = j.x[s][i][e]; // (a cast of the vector's element itself takes the first one)
+                const f16x2 v = __builtin_bit_cast(f16x2, two);
+                o[i][2 * e] = there ? fmaf((float)v[0], f, o[i][2 * e]) : o[i][2 * e];
+                o[i][2 * e + 1] = there ? fmaf((float)v[1], f, o[i][2 * e + 1]) : o[i][2 * e + 1];
+            }
+        }
+    }
+}
+// All of it: j holds the first N parts; on return o, G pieces from pc on, is to be divided by l.
+template <int N, int G>
+__device__ __forceinline__ void join_row(const SharedRow& r, int pc, JoinParts<N, G>& j, float m, float& l, float (&o)[G][8]) {
+    const float M = join_reference(r, j, m), f = __builtin_amdgcn_exp2f(m - M);
+    l *= f;
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[i][e] *= f;
+    join_parts(r, 0, pc, j, M, l, o);
+    for (int s0 = N; s0 < r.parts; s0 += N) {
+        load_parts(r, s0, pc, j);
+        join_parts(r, s0, pc, j, M, l, o);
+    }
+}
+// Statuses, by workgroups of their own behind the last one of the launch over the sequences' own keys, a wave a sequence: the trips of a report in a row, up
+// to the block ids, would otherwise be a tail of the workgroups that also compute. `first`: the first such workgroup's number.
+__device__ __forceinline__ void report_shared(const SharedParams& p, int first) {
+    const int lane = threadIdx.x & 63, b = ((int)blockIdx.x - first) * ((int)blockDim.x >> 6) + ((int)threadIdx.x >> 6);
+    if (!p.status || b >= p.B) return;
+    const int32_t parent = p.parent[(int64_t)b * p.T + min(lane, p.T - 1)], S = p.prefix_len[b], len = p.shared_len[0];
+    bool bad = false;
+    const bool s_ok = prefix_ok(p, S), ok = shared_ok(p, len);
+    if (p.paged && s_ok)
+        for (int i = lane; i < (S + p.tree_keys + p.block_size - 1) >> p.block_shift; i += kWave)
+            bad |= (uint32_t)p.block_table[(int64_t)b * p.max_blocks + i] >= (uint32_t)p.num_blocks;
+    if (p.shared_table && ok)
+        for (int i = lane; i < (len + (1 << p.sh_block_shift) - 1) >> p.sh_block_shift; i += kWave) bad |= (uint32_t)p.shared_table[i] >= (uint32_t)p.sh_num_blocks;
+    int32_t code = VS_STATUS_OK;
+    if (!p.tree_mask) {
+        if (__any(lane > 0 && lane < p.T && (parent < 0 || parent >= lane))) code = VS_STATUS_BAD_PARENT;
+        if (__any(lane == 0 && parent != -1)) code = VS_STATUS_BAD_ROOT;
+    }
+    if (code == VS_STATUS_OK && !(s_ok && ok)) code = VS_STATUS_BAD_PREFIX;
+    if (code == VS_STATUS_OK && __any(bad)) code = VS_STATUS_BAD_BLOCK;
+    if (lane == 0) p.status[b] = code;
 }
 
 } // namespace vs

@@ -87,16 +87,22 @@ struct AttnParams {
 // in fp32, and every sequence's rows against its own keys, joined with them.
 enum RowsMode { kRowsWhole = 0, kRowsShared = 1, kRowsOwn = 2 }; // the kernels of vs_tree_verify_attention, and these two
 struct SharedParams : AttnParams {
-    float* sh_acc;              // [KV head][split][row][d]: sums of weights times values, relative to the split's reference
-    float* sh_ml;               // [KV head][split][row][2]: reference (log2 domain), sum of weights
+    float* sh_acc;              // the parts' means (bf16 storage) or sums of weights times values, see attn_shared.h
+    float* sh_ml;               // [KV head][part][row]: reference (log2 domain), sum of weights; bf16 storage: and exponents
     const int32_t* shared_len;
     const int32_t* shared_table; // paged only
-    int32_t sh_rows;            // rows of all sequences: B * T * group
-    int32_t sh_splits, sh_keys_per_split;
+    int32_t sh_rows, sh_blocks; // rows of all sequences, B * T * group, and 32-row blocks of them
+    int32_t sh_splits, sh_keys_per_split; // places for parts of a row, at most; keys of one where the parts are equal splits
+    int32_t sh_shares;          // else the number of equal shares of all (KV head, row group) units' keys; 0: equal splits
+    int32_t sh_units, sh_groups; // units, and row groups of a KV head
+    FastDiv sh_by_rows;         // rows of a row group
     int32_t max_shared;
     int32_t sh_block_shift, sh_num_blocks; // paged only
     int64_t sh_slots;           // of the shared prefix's cache
 };
+
+// Grids of the kernels that deal workgroups over the XCDs.
+constexpr uint32_t round_up8(int32_t wgs) { return ((uint32_t)wgs + 7) / 8 * 8; }
 
 struct AcceptParams {
     const float* logits;
@@ -281,7 +287,8 @@ bool attention_resident_supported(int row_blocks);
 hipError_t launch_attention_mfma_resident(const AttnParams& p, int row_blocks, hipStream_t s);
 hipError_t launch_attention_mfma_rows(const AttnParams& p, int waves, hipStream_t s);
 hipError_t launch_attention_mfma_rounds(const AttnParams& p, int row_blocks, hipStream_t s);
-hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, hipStream_t s);
+hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, int waves, hipStream_t s);
+hipError_t launch_attention_shared_pipe(const SharedParams& p, RowsMode mode, int waves, hipStream_t s);
 hipError_t launch_attention_shared_f32(const SharedParams& p, RowsMode mode, hipStream_t s);
 hipError_t launch_attention_combine(const AttnParams& p, int dtype, hipStream_t s);
 hipError_t launch_accept(AcceptParams p, void* workspace, hipStream_t s);        // sets pairs, chunks
