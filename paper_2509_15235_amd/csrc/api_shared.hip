@@ -48,6 +48,7 @@ struct Cut {
 struct SharedPlan {
     Cut shared, own;
     int32_t own_waves, own_pipe;
+    int32_t steps, longer, per_line, line_steps; // of a share, of a line of shares
     int32_t waves, shares; // the pipelined kernel on equal shares of all row groups' keys; 0: own tiles, equal splits
     size_t acc_bytes, ml_bytes;
 };
@@ -59,15 +60,26 @@ SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
     const bool f32 = d->dtype == VS_F32;
     const int tiles = (prefix.max_prefix_len + kIterKeys - 1) / kIterKeys;
     Cut& s = pl.shared;
-    if (!f32 && rows > (getenv("PIPEROWS") ? atoi(getenv("PIPEROWS")) : 128)) {
+    if (!f32 && (int64_t)d->Hkv * ((rows + 255) / 256) * tiles <= 0x7fffffff && rows > (getenv("PIPEROWS") ? atoi(getenv("PIPEROWS")) : 128)) {
         pl.waves = getenv("W4") ? 4 : 8;
         s.rows_per_group = pl.waves * kRowBlock;
         s.row_groups = (int32_t)((rows + s.rows_per_group - 1) / s.rows_per_group);
         const int64_t units = (int64_t)d->Hkv * s.row_groups, steps = units * tiles, places = kNumCUs * (pl.waves == 8 ? 1 : 2);
-        pl.shares = (int32_t)(steps / 4 < places ? (steps + 3) / 4 : places);
-        if (pl.shares < units && pl.shares < places) pl.shares = (int32_t)(units < places ? units : places);
+        // Shares anywhere: all CUs end together, but a share that ends one unit and begins another pays for two beginnings and ends, 8 steps' time or so each.
+        // Or every unit in the same number of them.
+        int64_t shares = steps / 4 < places ? (steps + 3) / 4 : places, whole = places / units;
+        if (whole > tiles / 4) whole = tiles / 4;
+        if (whole < 1) whole = 1;
+        const int64_t any = (steps + shares - 1) / shares + 9, even = ((tiles + whole - 1) / whole + 4) * ((units * whole + places - 1) / places);
+        const bool lines = even <= any;
+        const int64_t per = lines ? whole : shares, line = lines ? tiles : steps;
+        pl.shares = (int32_t)(lines ? units * whole : shares);
+        pl.per_line = (int32_t)per;
+        pl.line_steps = (int32_t)line;
+        pl.steps = (int32_t)(line / per);
+        pl.longer = (int32_t)(line % per);
         // a unit's steps begin in one share and end in another: at most so many
-        s.num_splits = (int32_t)((pl.shares + units - 1) / units) + 1;
+        s.num_splits = lines ? (int32_t)whole : (int32_t)((tiles + pl.steps - 1) / pl.steps) + 1;
         s.keys_per_split = kIterKeys;
         s.total_wgs = pl.shares;
     } else {
@@ -124,9 +136,17 @@ SharedParams shared_params(const AttnParams& base, const Cut& c, const SharedPla
     p.sh_splits = pl.shared.num_splits;
     p.sh_keys_per_split = pl.shared.keys_per_split;
     p.sh_shares = pl.shares;
+    p.sh_steps = pl.steps;
+    p.sh_longer = pl.longer;
     p.sh_groups = pl.shared.row_groups;
-    p.sh_units = d->Hkv * pl.shared.row_groups;
     p.sh_by_rows = fast_div_by(pl.shared.rows_per_group);
+    p.sh_by_steps = fast_div_by((prefix.max_prefix_len + kIterKeys - 1) / kIterKeys);
+    if (pl.shares) {
+        p.sh_by_line = fast_div_by(pl.per_line);
+        p.sh_by_line_steps = fast_div_by(pl.line_steps);
+        p.sh_by_share = fast_div_by(pl.steps);
+        p.sh_by_longer = fast_div_by(pl.steps + 1);
+    }
     p.max_shared = prefix.max_prefix_len;
     while (prefix.paged && (1 << p.sh_block_shift) < prefix.block_size) ++p.sh_block_shift;
     p.sh_num_blocks = prefix.num_blocks;

@@ -41,7 +41,7 @@ template <int D, int RPW, int NW, bool PAGED, bool BAL, bool ONCE, int MODE = kR
 __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma_pipe_kernel(const std::conditional_t<MODE == kRowsWhole, AttnParams, SharedParams> p) {
     request_args(p);
     constexpr bool SHARED = MODE == kRowsShared, OWN = MODE == kRowsOwn;
-    constexpr bool PIECES = BAL || SHARED; // a workgroup has several pieces of work, and knows the sequences' lengths
+    constexpr bool PIECES = BAL || SHARED; // a workgroup has several pieces of work
     constexpr int KS = D / 16;                 // k-steps of the S^T product
     constexpr int DB = D / 32;                 // 32-channel blocks of the output
     constexpr int SUB = kTileKeys * D;         // elements per 32-key tile of K (or V)
@@ -117,8 +117,8 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     // (Before, the wave waited for the length, and paged for the queries, before it asked for the tiles: us per layer, 28 / 4 heads, before /
     // so: 6 x 60 nodes, 2044 .. 4089 keys paged 33.2 / 32.3; 6 x 23, 903 .. 1806 keys 17.9 / 17.4; longer launches 0 - 1 %.)
     int32_t S = S_known;
-    if constexpr (DIRECT && !PIECES) load_to_lds4((uint32_t)(uintptr_t)(lds_void*)&sLen[wave][0], p.prefix_len + b, 0u);
-    else if constexpr (!PIECES) S = p.prefix_len[b];
+    if constexpr (DIRECT && !BAL) load_to_lds4((uint32_t)(uintptr_t)(lds_void*)&sLen[wave][0], p.prefix_len + b, 0u);
+    else if constexpr (!BAL) S = p.prefix_len[b];
 
     // ---- tile copies. One load instruction of a wave fetches 1 KB of consecutive memory:
     // RPI whole rows (tokens) of D channels, lane q -> row q / LPR, 16-byte chunk q % LPR, so
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     // table's). Values of rows that turn out to lie past the sequence's last key become zeros in LDS (DIRECT: zero_tail) or on their way there from register set 1: whatever the cache holds there, NaN included,
     // must not meet a zero probability.
     if constexpr (EARLY) {
-        const int kend = early_end(PIECES ? S_known + p.tree_keys : most_keys(p), k0, klen);
+        const int kend = early_end(BAL ? S_known + p.tree_keys : most_keys(p), k0, klen);
         if constexpr (DIRECT) rows_up_to(kend);
         auto load_tile_early = [&](auto is_v, int t, u32x4(&r)[BPW]) __attribute__((always_inline)) {
             const uint16_t* gbase = decltype(is_v)::value ? vbase : kbase;
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     } else {
         tree_code = load_tree(p.parent + (int64_t)b * p.T, p.T, sp, &sflag);
     }
-    if constexpr (DIRECT && !PIECES) {
+    if constexpr (DIRECT && !BAL) {
         // loads behind it: those above, the fewest of any wave
         constexpr int TILES_K = Q_K < NSLOT - 1 ? Q_K : NSLOT - 1;
         wait_loads<(PAGED ? 2 : 0) + KS + (HALVES ? (TILES_K < Q_V ? TILES_K : Q_V) : TILES_K + Q_V)>();
@@ -961,18 +961,14 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
 
     if constexpr (SHARED) {
         // workgroup -> share; consecutive shares, which read neighbouring keys of one KV head, on one XCD
-        const int w = (int)((blockIdx.x & 7) * (uint32_t)((p.sh_shares + 7) >> 3) + (blockIdx.x >> 3));
-        const int32_t len = p.shared_len[0];
-        if (w >= p.sh_shares || !shared_ok(p, len) || len == 0) return;
-        const uint32_t steps = (uint32_t)(len + kIterKeys - 1) / kIterKeys;
-        const uint64_t total = (uint64_t)p.sh_units * steps;
-        const uint64_t hi = share_begin(p, total, w + 1);
-        for (uint64_t lo = share_begin(p, total, w); lo < hi;) {
-            const uint32_t u = __builtin_amdgcn_readfirstlane((uint32_t)(lo / steps)), t0 = __builtin_amdgcn_readfirstlane((uint32_t)(lo - (uint64_t)u * steps));
-            const uint32_t t1 = __builtin_amdgcn_readfirstlane((uint32_t)min((uint64_t)steps, t0 + (hi - lo)));
-            uint32_t rg;
+        const int w = (int)((blockIdx.x & 7) * (round_up8(p.sh_shares) >> 3) + (blockIdx.x >> 3));
+        if (w >= p.sh_shares) return;
+        const uint32_t hi = share_begin(p, (uint32_t)w + 1);
+        for (uint32_t lo = share_begin(p, (uint32_t)w); lo < hi;) {
+            uint32_t rg, t0;
+            const uint32_t u = fast_div(lo, p.sh_by_steps, t0), t1 = min(p.sh_by_steps.d, t0 + (hi - lo));
             const int kvh = (int)fast_div(u, p.by_groups, rg);
-            run_piece(0, kvh, (int)rg, (int)t0 * kIterKeys, (int)(t1 - t0) * kIterKeys, w - first_share(p, total, steps, u), false, len);
+            run_piece(0, kvh, (int)rg, (int)t0 * kIterKeys, (int)(t1 - t0) * kIterKeys, w - share_of(p, u * p.sh_by_steps.d), false, 0);
             lo += t1 - t0;
             if (lo < hi) __syncthreads(); // the last reads of the tile rings
         }

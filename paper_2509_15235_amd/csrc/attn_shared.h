@@ -14,22 +14,30 @@ namespace vs {
 
 __device__ __forceinline__ bool shared_ok(const SharedParams& p, int32_t len) { return len >= 0 && len <= p.max_shared && len <= p.sh_slots; }
 
-// ---- Equal shares: all units - (KV head, row group), a KV head's next to each other - have the same `steps` of 64 keys, laid end to end; share w
-// takes the steps from w * total / shares on. A unit's parts are the pieces of consecutive shares.
-__device__ __forceinline__ uint64_t share_begin(const SharedParams& p, uint64_t total, int w) { return (uint64_t)w * total / (uint32_t)p.sh_shares; }
-// the share that step x lies in: the largest w with w * total / shares <= x
-__device__ __forceinline__ int share_of(const SharedParams& p, uint64_t total, uint64_t x) { return (int)(((x + 1) * (uint32_t)p.sh_shares - 1) / total); }
-__device__ __forceinline__ int first_share(const SharedParams& p, uint64_t total, uint32_t steps, uint32_t unit) { return share_of(p, total, (uint64_t)unit * steps); }
+// ---- Shares: a unit - (KV head, row group) - has as many steps of 64 keys as the longest allowed prefix; all units lie end to end in one line that is
+// cut into shares, or each in a line of its own. The first sh_longer shares of a line take sh_steps + 1 steps, the others sh_steps. A unit's
+// parts are the pieces of consecutive shares. (By the host's bound, not by the length: the divisions that the length would take, and the trip for
+// it, stood in front of every first tile.)
+__device__ __forceinline__ uint32_t share_begin(const SharedParams& p, uint32_t w) { // of a line's last share + 1: the next line's begin
+    uint32_t i;
+    const uint32_t line = fast_div(w, p.sh_by_line, i);
+    return line * p.sh_by_line_steps.d + i * (uint32_t)p.sh_steps + min(i, (uint32_t)p.sh_longer);
+}
+__device__ __forceinline__ int share_of(const SharedParams& p, uint32_t step) {
+    const uint32_t longer = (uint32_t)p.sh_longer * (uint32_t)(p.sh_steps + 1);
+    uint32_t x, rest;
+    const uint32_t line = fast_div(step, p.sh_by_line_steps, x);
+    return (int)(line * p.sh_by_line.d + (x < longer ? fast_div(x, p.sh_by_longer, rest) : (uint32_t)p.sh_longer + fast_div(x - longer, p.sh_by_share, rest)));
+}
 
 // How many parts there are of a row against the shared keys (none where their number is not one, which is reported, or zero).
 __device__ __forceinline__ int shared_parts(const SharedParams& p, int32_t len, int kvh, int row) {
     if (!shared_ok(p, len) || len == 0) return 0;
     if (p.sh_shares == 0) return (len + p.sh_keys_per_split - 1) / p.sh_keys_per_split;
     const uint32_t steps = (uint32_t)(len + kIterKeys - 1) / kIterKeys;
-    const uint64_t total = (uint64_t)p.sh_units * steps;
     uint32_t rest;
-    const uint32_t unit = (uint32_t)kvh * p.sh_groups + fast_div((uint32_t)row, p.sh_by_rows, rest);
-    return share_of(p, total, (uint64_t)(unit + 1) * steps - 1) - first_share(p, total, steps, unit) + 1;
+    const uint32_t first = ((uint32_t)kvh * p.sh_groups + fast_div((uint32_t)row, p.sh_by_rows, rest)) * p.sh_by_steps.d;
+    return share_of(p, first + steps - 1) - share_of(p, first) + 1;
 }
 // Number of (KV head, part, row). fp32 storage: its pair (m, l) and its d sums of weights times values lie there.
 __device__ __forceinline__ int64_t shared_row(const SharedParams& p, int kvh, int part, int row) {

@@ -93,9 +93,11 @@ struct SharedParams : AttnParams {
     const int32_t* shared_table; // paged only
     int32_t sh_rows, sh_blocks; // rows of all sequences, B * T * group, and 32-row blocks of them
     int32_t sh_splits, sh_keys_per_split; // places for parts of a row, at most; keys of one where the parts are equal splits
-    int32_t sh_shares;          // else the number of equal shares of all (KV head, row group) units' keys; 0: equal splits
-    int32_t sh_units, sh_groups; // units, and row groups of a KV head
-    FastDiv sh_by_rows;         // rows of a row group
+    int32_t sh_shares;          // else the number of shares of all (KV head, row group) units' keys, 0: equal splits
+    int32_t sh_steps, sh_longer; // steps of 64 keys of a share, and how many shares of a line have one more
+    FastDiv sh_by_line, sh_by_line_steps; // shares and steps of a line
+    int32_t sh_groups;          // row groups of a KV head
+    FastDiv sh_by_rows, sh_by_steps, sh_by_share, sh_by_longer; // rows of a row group, steps of a unit, sh_steps, sh_steps + 1
     int32_t max_shared;
     int32_t sh_block_shift, sh_num_blocks; // paged only
     int64_t sh_slots;           // of the shared prefix's cache
