@@ -48,9 +48,11 @@ struct Cut {
 struct SharedPlan {
     Cut shared, own;
     int32_t own_waves, own_pipe;
+    int32_t both;   // one launch
+    int32_t places; // for parts of a row
     int32_t steps, longer, per_line, line_steps; // of a share, of a line of shares
     int32_t waves, shares; // the pipelined kernel on equal shares of all row groups' keys; 0: own tiles, equal splits
-    size_t acc_bytes, ml_bytes;
+    size_t acc_bytes, ml_bytes, word_bytes;
 };
 
 SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
@@ -83,17 +85,21 @@ SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
         s.keys_per_split = kIterKeys;
         s.total_wgs = pl.shares;
     } else {
-    s.rows_per_group = f32 ? 8 : d->d == 128 && rows > kRowBlock ? 2 * kRowBlock : kRowBlock;
-    s.row_groups = (int32_t)((rows + s.rows_per_group - 1) / s.rows_per_group);
-    const int64_t wgs = (int64_t)d->Hkv * s.row_groups;
-    int64_t splits = kNumCUs / wgs;
-    if (splits > (tiles + 3) / 4) splits = (tiles + 3) / 4;
-    if (splits > kMergeMaxSplits) splits = kMergeMaxSplits;
-    if (splits < 1) splits = 1;
-    const int tps = (int)((tiles + splits - 1) / splits);
-    s.keys_per_split = tps * kIterKeys;
-    s.num_splits = (tiles + tps - 1) / tps;
-    s.total_wgs = (int32_t)(wgs * s.num_splits);
+        // One launch for both kinds of work where all workgroups run at once (and one row block of the shared keys to a workgroup): us per call,
+        // two launches / one
+        const int64_t blocks = (rows + kRowBlock - 1) / kRowBlock, own = (int64_t)d->B * d->Hkv;
+        pl.both = !f32 && d->T * group <= kRowBlock && (d->paged != 0) == (prefix.paged != 0) && own + blocks * d->Hkv <= kNumCUs && !getenv("NOBOTH");
+        s.rows_per_group = f32 ? 8 : d->d == 128 && rows > kRowBlock && !pl.both ? 2 * kRowBlock : kRowBlock;
+        s.row_groups = (int32_t)((rows + s.rows_per_group - 1) / s.rows_per_group);
+        const int64_t wgs = (int64_t)d->Hkv * s.row_groups;
+        int64_t splits = (kNumCUs - (pl.both ? own : 0)) / wgs;
+        if (splits > (tiles + 3) / 4) splits = (tiles + 3) / 4;
+        if (splits > kMergeMaxSplits) splits = kMergeMaxSplits;
+        if (splits < 1) splits = 1;
+        const int tps = (int)((tiles + splits - 1) / splits);
+        s.keys_per_split = tps * kIterKeys;
+        s.num_splits = (tiles + tps - 1) / tps;
+        s.total_wgs = (int32_t)(wgs * s.num_splits);
     }
     Cut& o = pl.own;
     const int own_rows = d->T * group;
@@ -107,11 +113,13 @@ SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
     o.num_splits = 1;
     o.keys_per_split = (int32_t)(((int64_t)d->max_prefix_len + d->T + kIterKeys - 1) / kIterKeys * kIterKeys);
     o.total_wgs = d->B * d->Hkv * o.row_groups;
-    if (!pl.own_pipe) pl.own_waves = o.rows_per_group > kRowBlock || o.total_wgs <= kNumCUs ? 8 : o.total_wgs <= 2 * kNumCUs ? 4 : 2;
-    const size_t parts = (size_t)d->Hkv * s.num_splits;
+    if (!pl.own_pipe) pl.own_waves = o.rows_per_group > kRowBlock || o.total_wgs <= kNumCUs ? 8 : d->d == 64 ? 2 : 4;
+    pl.places = s.num_splits + (pl.both ? 1 : 0);
+    const size_t parts = (size_t)d->Hkv * pl.places;
     const size_t padded = (rows + kRowBlock - 1) / kRowBlock * kRowBlock; // whole row blocks
     pl.acc_bytes = align_up(parts * (f32 ? rows * d->d * sizeof(float) : padded * d->d * sizeof(uint16_t)));
     pl.ml_bytes = align_up(parts * rows * (f32 ? 2 : 4) * sizeof(float));
+    if (pl.both) pl.word_bytes = (size_t)d->B * d->Hkv * kArrivalWords * sizeof(uint64_t);
     return pl;
 }
 
@@ -129,11 +137,14 @@ SharedParams shared_params(const AttnParams& base, const Cut& c, const SharedPla
     p.by_heads = fast_div_by(d->Hkv);
     p.sh_acc = (float*)workspace;
     p.sh_ml = (float*)((char*)workspace + pl.acc_bytes);
+    p.sh_words = (uint64_t*)((char*)p.sh_ml + pl.ml_bytes);
     p.shared_len = shared_len;
     p.shared_table = prefix.paged ? prefix.block_table : nullptr;
+    p.sh_batch = d->B;
+    p.sh_own_rows = d->T * (d->Hq / d->Hkv);
     p.sh_rows = d->B * d->T * (d->Hq / d->Hkv);
     p.sh_blocks = (p.sh_rows + kRowBlock - 1) / kRowBlock;
-    p.sh_splits = pl.shared.num_splits;
+    p.sh_splits = pl.places;
     p.sh_keys_per_split = pl.shared.keys_per_split;
     p.sh_shares = pl.shares;
     p.sh_steps = pl.steps;
@@ -162,7 +173,7 @@ size_t vs_shared_prefix_workspace_bytes(const vs_attn_desc* desc, const vs_prefi
     vs_attn_desc x;
     if (check_shared(desc, prefix, x) != VS_OK) return 0;
     const SharedPlan pl = plan_shared(desc, x);
-    return pl.acc_bytes + pl.ml_bytes;
+    return pl.acc_bytes + pl.ml_bytes + pl.word_bytes;
 }
 
 int32_t vs_shared_prefix_attention(const vs_attn_desc* desc, const vs_prefix_desc* prefix, const void* q, const void* k_shared, const void* v_shared,
@@ -175,7 +186,7 @@ int32_t vs_shared_prefix_attention(const vs_attn_desc* desc, const vs_prefix_des
     for (const void* at : {q, k_shared, v_shared, k_cache, v_cache, (const void*)out})
         if (!aligned16(at)) return VS_ERR_LAYOUT;
     const SharedPlan pl = plan_shared(desc, x);
-    if (!workspace || workspace_bytes < pl.acc_bytes + pl.ml_bytes || ((uintptr_t)workspace & (kAlign - 1))) return VS_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < pl.acc_bytes + pl.ml_bytes + pl.word_bytes || ((uintptr_t)workspace & (kAlign - 1))) return VS_ERR_WORKSPACE;
     if (const int32_t dc = check_device()) return dc;
     hipStream_t s = (hipStream_t)stream;
     const bool f32 = desc->dtype == VS_F32;
@@ -183,6 +194,7 @@ int32_t vs_shared_prefix_attention(const vs_attn_desc* desc, const vs_prefix_des
                                              shared_len, workspace);
     const SharedParams second = shared_params(attention_params(desc, 1, q, k_cache, v_cache, prefix_len, tree_parent, tree_mask, out, status), pl.own, pl, desc, x,
                                               shared_len, workspace);
+    if (pl.both) return launch_attention_shared_both(first, second, s) == hipSuccess ? VS_OK : VS_ERR_HIP;
     hipError_t e = f32 ? launch_attention_shared_f32(first, kRowsShared, s) : pl.waves ? launch_attention_shared_pipe(first, kRowsShared, pl.waves, s) : launch_attention_shared_rows(first, kRowsShared, 8, s);
     if (e == hipSuccess) e = f32 ? launch_attention_shared_f32(second, kRowsOwn, s) : pl.own_pipe ? launch_attention_shared_pipe(second, kRowsOwn, pl.own_waves, s) : launch_attention_shared_rows(second, kRowsOwn, pl.own_waves, s);
     return e == hipSuccess ? VS_OK : VS_ERR_HIP;

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const st
     // the row groups of a unit run on one XCD and share its L2 (one split)
     if constexpr (MODE == kRowsOwn)
         if (blockIdx.x >= round_up8(p.total_wgs)) {
-            report_shared(p, (int)round_up8(p.total_wgs));
+            report_shared(p, round_up8(p.total_wgs));
             return;
         }
     const WorkItem at = work_item(p);

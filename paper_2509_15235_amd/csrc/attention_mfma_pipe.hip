@@ -975,7 +975,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     } else if constexpr (!BAL) {
         if constexpr (OWN)
             if (blockIdx.x >= round_up8(p.total_wgs)) {
-                report_shared(p, (int)round_up8(p.total_wgs));
+                report_shared(p, round_up8(p.total_wgs));
                 return;
             }
         int b, kvh, rg, split = 0;

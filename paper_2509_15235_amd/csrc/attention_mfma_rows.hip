@@ -31,10 +31,22 @@ namespace {
 // ONCE: tiles as data that is read once (the host's rule says when). Part of the kernel as well: a branch at every load 5 % of two row blocks'
 // time, a loop of its own for either kind 3 % of a short call's.
 // CROWD: many splits on nearly all CUs, whose workgroups wait for each other at another word (merge_meet).
-// MODE: kRowsShared, all sequences' rows against the keys that they share (one sequence of B * T nodes, no tree slots), whose results stay
-// partial ones in fp32; kRowsOwn, a sequence's rows against its own keys, joined with those (attn_shared.h).
+// MODE (attn_shared.h): kRowsShared, all sequences' rows against the keys that they share (one sequence of B * T nodes, no tree slots), whose results stay
+// partial ones; kRowsOwn, a sequence's rows against its own keys, joined with those;
+// kRowsBoth, workgroups of either kind in one launch, and those that report.
+struct BothParams {
+    SharedParams work[2]; // the sequences' own keys, the shared ones
+};
+template <int MODE>
+using RowsArgs = std::conditional_t<MODE == kRowsWhole, AttnParams, std::conditional_t<MODE == kRowsBoth, BothParams, SharedParams>>;
+template <int MODE>
+__device__ __forceinline__ const auto& rows_params(const RowsArgs<MODE>& args, bool shared_work) {
+    // (out of the arguments' own place: an element of a local copy that is chosen at run time would have the copy in scratch memory)
+    if constexpr (MODE == kRowsBoth) return *((const SharedParams*)(const void*)__builtin_amdgcn_kernarg_segment_ptr() + (shared_work ? 1 : 0));
+    else return args;
+}
 template <int D, int NW, int RB, bool PAGED, bool ONCE, bool CROWD = false, int MODE = kRowsWhole>
-__global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::conditional_t<MODE == kRowsWhole, AttnParams, SharedParams> p) {
+__global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const RowsArgs<MODE> args) {
     constexpr int KS = D / 16;          // k-steps of the S^T product
     constexpr int DB = D / 32;          // 32-channel blocks of the output
     constexpr int SUB = kTileKeys * D;  // elements per 32-key tile of K (or V)
@@ -54,6 +66,21 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
     __shared__ __attribute__((aligned(1024))) uint16_t smem[SMEM_ELEMS];
     __shared__ int32_t sp[VS_MAX_TREE];
     __shared__ int32_t sflag;
+
+    // kRowsBoth: the workgroups of the shared keys come first; what this one works on, and its number there
+    constexpr bool BOTH = MODE == kRowsBoth;
+    bool shared_work = MODE == kRowsShared;
+    uint32_t id = blockIdx.x;
+    if constexpr (BOTH) {
+        const uint32_t first = round_up8(args.work[1].total_wgs), end = first + round_up8(args.work[0].total_wgs);
+        shared_work = id < first;
+        if (id >= end) {
+            report_shared(args.work[0], end);
+            return;
+        }
+        if (!shared_work) id -= first;
+    }
+    const auto& p = rows_params<MODE>(args, shared_work);
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
@@ -75,10 +102,10 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
     } else {
         if constexpr (MODE == kRowsOwn)
             if (blockIdx.x >= round_up8(p.total_wgs)) {
-                report_shared(p, (int)round_up8(p.total_wgs));
+                report_shared(p, round_up8(p.total_wgs));
                 return;
             }
-        const WorkItem at = work_item(p);
+        const WorkItem at = work_item(p, id);
         if (at.none) return;
         b = at.b;
         kvh = at.kvh;
@@ -174,10 +201,21 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
     constexpr int EARLY = MODE == kRowsOwn ? (PPW == 1 ? 8 : 4) : 1;
     JoinParts<EARLY, PPW> parts; // (two row blocks have no registers for them yet)
     SharedRow joined[MODE == kRowsOwn ? RB : 1];
-    int32_t shared = 0;
     const int my_piece = min(wave, NP / PPW - 1) * PPW;
-    if constexpr (MODE == kRowsOwn) {
-        shared = p.shared_len[0];
+    // kRowsBoth: how many parts of the shared keys there are; wave 0: the sequence whose word the lane arrives at, and what that holds
+    int live = 0, to_b = -1;
+    uint64_t seen_own = 0;
+    if constexpr (BOTH) {
+        if (wave == 0) {
+            const int at = shared_work ? row0 / p.sh_own_rows + lane : b;
+            if (at < p.sh_batch && (shared_work ? at * p.sh_own_rows < row0 + kRowBlock : lane == 0)) {
+                to_b = at;
+                seen_own = load_device(own_word(p, kvh, at));
+            }
+        }
+        live = shared_parts(p, p.shared_len[0], kvh, 0);
+    } else if constexpr (MODE == kRowsOwn) {
+        const int32_t shared = p.shared_len[0];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             joined[rb] = shared_at<D>(p, shared, kvh, b * p.rows + min(row0 + rb * kRowBlock + col, p.rows - 1), half);
@@ -201,12 +239,19 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
         }
     }
     const bool s_ok = prefix_ok(p, S);
-    if constexpr (MODE != kRowsOwn)
+    if constexpr (MODE != kRowsOwn && !BOTH)
         if (kvh == 0 && split == 0 && rg == 0) report_status<PAGED>(p, b, tree_code, s_ok, S, &sflag);
-    if (tree_code != VS_STATUS_OK || !s_ok) return;
+    if (tree_code != VS_STATUS_OK || !s_ok) {
+        if constexpr (BOTH) // a sequence's rows are lost then, but the others count on its arrival
+            if (!shared_work && live > 0 && to_b >= 0) {
+                arrival_open(own_word(p, kvh, b), seen_own);
+                (void)arrival_last(own_word(p, kvh, b), own_parties(p, b, live));
+            }
+        return;
+    }
     const int nk = S + p.tree_keys;
     if (k0 >= nk) return;
-    const bool final_rows = MODE == kRowsOwn || p.num_splits == 1 || (p.gates && nk <= p.keys_per_split); // a sequence of one split has nothing to merge
+    const bool final_rows = MODE == kRowsOwn || BOTH || p.num_splits == 1 || (p.gates && nk <= p.keys_per_split); // a sequence of one split has nothing to merge
     const bool merge = MODE == kRowsWhole && p.gates && !final_rows;
     if (merge && tid == 0) [[unlikely]] merge_open(gate, seen); // (most waves only jump over it)
     const int k1 = min(nk, k0 + p.keys_per_split);
@@ -408,7 +453,13 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
             float inv = l > 0.f ? 1.f / l : 0.f; // no visible key in this split (partials only): zeros, weight 0
             if constexpr (MODE != kRowsWhole) {
                 const int row = row0 + rb * kRowBlock + col;
-                if constexpr (MODE == kRowsShared) {
+                if constexpr (BOTH) {
+                    if (shared_work || live > 0) {
+                        if (row < p.rows) // (both halves of a row)
+                            store_part<D>(p, kvh, shared_work ? split : p.sh_splits - 1, shared_work ? row : b * p.rows + row, half, my_piece, wave == 0, M, l, r);
+                        continue;
+                    }
+                } else if constexpr (MODE == kRowsShared) {
                     if (row >= p.rows) continue; // (both halves of a row)
                     char* const to = shared_means<D>(p, kvh, split, row, half);
                     char* const head = shared_head(p, kvh, split, row);
@@ -456,6 +507,31 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const std::c
             }
         }
     }
+    if constexpr (BOTH) {
+        static_assert(RB == 1, "one row block");
+        if (live == 0) return; // no shared keys: the own rows are written
+        __builtin_amdgcn_s_waitcnt(wait_vm(0)); // this wave's part is in memory
+        __syncthreads();
+        if (wave == 0) {
+            bool last = false;
+            if (to_b >= 0) {
+                arrival_open(own_word(p, kvh, to_b), seen_own);
+                last = arrival_last(own_word(p, kvh, to_b), own_parties(p, to_b, live));
+            }
+            const uint32_t which = (uint32_t)__ballot(last); // (a row block has at most 32 sequences)
+            if (lane == 0) sflag = (int32_t)which;
+        }
+        __syncthreads();
+        const uint32_t todo = (uint32_t)sflag;
+        if (todo == 0) return;
+        // 32 rows at a time: of this row block, and what its first and last sequence have in the ones beside it
+        const int first_b = shared_work ? row0 / p.sh_own_rows : b;
+        const int from = (first_b + __builtin_ctz(todo)) * p.sh_own_rows, to = (first_b + 32 - __builtin_clz(todo)) * p.sh_own_rows;
+        for (int at = shared_work ? from / kRowBlock * kRowBlock : from; at < to; at += kRowBlock) {
+            const int row = at + col, which = row / p.sh_own_rows - first_b;
+            join_rows<D, NW>(args.work[0], kvh, live, row, row >= from && row < to && ((todo >> which) & 1) != 0);
+        }
+    }
     if constexpr (MODE == kRowsWhole)
         if (merge) merge_splits<D, CROWD>(p, gate, b, kvh, block0, block0 + RB, split, (nk + p.keys_per_split - 1) / p.keys_per_split, NW, (uint32_t*)sp);
 }
@@ -489,6 +565,24 @@ hipError_t launch_shared_own(const SharedParams& p, int waves, hipStream_t s) {
 }
 
 } // namespace
+
+namespace {
+template <int D, int NW>
+hipError_t launch_both(const BothParams& p, hipStream_t s) {
+    const SharedParams& own = p.work[0];
+    const dim3 grid(round_up8(p.work[1].total_wgs) + round_up8(own.total_wgs) + (own.status ? (own.B + NW - 1) / NW : 0)), block(NW * kWave);
+    if (own.paged) hipLaunchKernelGGL((attn_mfma_rows_kernel<D, NW, 1, true, false, false, kRowsBoth>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((attn_mfma_rows_kernel<D, NW, 1, false, false, false, kRowsBoth>), grid, block, 0, s, p);
+    return hipGetLastError();
+}
+} // namespace
+
+hipError_t launch_attention_shared_both(const SharedParams& shared, const SharedParams& own, hipStream_t s) {
+    if (shared.rows_per_group != kRowBlock || own.rows > kRowBlock || own.row_groups != 1 || own.num_splits != 1 || shared.paged != own.paged) return hipErrorInvalidValue;
+    if ((own.d != 64 && own.d != 128) || shared.sh_splits != shared.num_splits + 1) return hipErrorInvalidValue;
+    const BothParams p{{own, shared}};
+    return own.d == 128 ? launch_both<128, 8>(p, s) : launch_both<64, 8>(p, s);
+}
 
 hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, int waves, hipStream_t s) {
     const int blocks = p.rows_per_group / kRowBlock;

@@ -100,12 +100,13 @@ struct WorkItem {
     int b, kvh, rg, split;
     bool none; // the last workgroups of a launch that is no multiple of eight
 };
-__device__ __forceinline__ WorkItem work_item(const AttnParams& p) {
-    const uint32_t v = (blockIdx.x & 7) * (uint32_t)((p.total_wgs + 7) >> 3) + (blockIdx.x >> 3);
+__device__ __forceinline__ WorkItem work_item(const AttnParams& p, uint32_t id) {
+    const uint32_t v = (id & 7) * (uint32_t)((p.total_wgs + 7) >> 3) + (id >> 3);
     uint32_t split, rg, kvh;
     const uint32_t b = fast_div(fast_div(fast_div(v, p.by_splits, split), p.by_groups, rg), p.by_heads, kvh);
     return {(int)b, (int)kvh, (int)rg, (int)split, v >= (uint32_t)p.total_wgs};
 }
+__device__ __forceinline__ WorkItem work_item(const AttnParams& p) { return work_item(p, blockIdx.x); }
 
 __device__ __forceinline__ int row_node(const AttnParams& p, int r) { return node_of_row(r, p.group, p.inv_group); }
 // the nodes of N rows, behind one branch

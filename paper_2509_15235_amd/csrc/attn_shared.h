@@ -151,10 +151,92 @@ __device__ __forceinline__ void join_row(const SharedRow& r, int pc, JoinParts<N
         join_parts(r, s0, pc, j, M, l, o);
     }
 }
+// ---- One launch for both kinds of work, where all workgroups run at once: parts then travel between them by stores and loads of device scope, and whoever
+// comes last joins. A sequence's own part has the last place of its rows. Nobody waits: every workgroup of a row block of the shared keys arrives at the
+// words of all sequences with rows in it, and so does each sequence's own workgroup; the last one at a sequence's word joins its rows.
+template <int D>
+__device__ __forceinline__ uint32_t means_offset(const SharedParams& p, int kvh, int part, int row, int half) { // bytes; the host keeps them below 2^31
+    return (uint32_t)(shared_means<D>(p, kvh, part, row, half) - (char*)p.sh_acc);
+}
+__device__ __forceinline__ uint32_t head_offset(const SharedParams& p, int kvh, int part, int row) { return (uint32_t)shared_row(p, kvh, part, row) * 16; }
+__device__ __forceinline__ uint64_t* own_word(const SharedParams& p, int kvh, int b) { return p.sh_words + (int64_t)kArrivalWords * (b * p.Hkv + kvh); }
+// Who arrives at the word of sequence b: `live` parts of every row block that its rows lie in, and its own workgroup.
+__device__ __forceinline__ uint32_t own_parties(const SharedParams& p, int b, int live) {
+    const int first = b * p.sh_own_rows;
+    return (uint32_t)((first + p.sh_own_rows - 1) / kRowBlock - first / kRowBlock + 1) * (uint32_t)live + 1;
+}
+// G pieces of part `part` of a row from pc on, and m, l and exponents (by wave 0: of the whole row)
+template <int D, int G>
+__device__ __forceinline__ void store_part(const SharedParams& p, int kvh, int part, int row, int half, int pc, bool heads, float m, float l, const float (&r)[G][8]) {
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const uint32_t to = means_offset<D>(p, kvh, part, row, half), head = head_offset(p, kvh, part, row);
+#pragma unroll
+    for (int i = 0; i < G; ++i) {
+        float mean[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mean[e] = r[i][e] * inv;
+        uint32_t exponent;
+        const u32x4 w = pack_means(mean, exponent);
+        __builtin_amdgcn_raw_buffer_store_b128(w, span_of(p.sh_acc), to + (pc + i) * 1024, 0, kDeviceScope);
+        if (half == 0) __builtin_amdgcn_raw_buffer_store_b8((uint8_t)exponent, span_of(p.sh_ml), head + 8 + pc + i, 0, kDeviceScope);
+    }
+    if (heads && half == 0) __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(m), __float_as_uint(l)}, span_of(p.sh_ml), head, 0, kDeviceScope);
+}
+// A row a lane (the same in both halves; rows counted over all sequences) out of all its parts, `parts` of the shared keys and the own one; each wave its
+// pieces. p: of the sequences' own keys. Rows that are not `active` are left alone.
+template <int D, int NW>
+__device__ __forceinline__ void join_rows(const SharedParams& p, int kvh, int parts, int row, bool active) {
+    constexpr int NP = D / 16, PPW = NP / NW > 0 ? NP / NW : 1, N = PPW == 1 ? 8 : 4;
+    const int half = (threadIdx.x >> 5) & 1, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    if (wave * PPW >= NP) return;
+    row = min(row, p.sh_rows - 1);
+    const int pc = wave * PPW, place = p.sh_splits - 1;
+    const uint32_t head0 = head_offset(p, kvh, 0, row), from0 = means_offset<D>(p, kvh, 0, row, half);
+    const uint32_t head_step = (uint32_t)p.sh_rows * 16, step = (uint32_t)p.sh_blocks * (kRowBlock * D * 2);
+    float M = -INFINITY, l = 0.f, o[PPW][8];
+#pragma unroll
+    for (int i = 0; i < PPW; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[i][e] = 0.f;
+    SharedRow all{parts + 1, nullptr, nullptr, 0, 0};
+    for (int s0 = 0; s0 <= parts; s0 += N) {
+        JoinParts<N, PPW> j;
+#pragma unroll
+        for (int s = 0; s < N; ++s) { // the own part behind the others; past it again
+            const uint32_t part = s0 + s < parts ? s0 + s : place;
+            j.head[s] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(span_of(p.sh_ml), head0 + part * head_step, 0, kDeviceScope));
+#pragma unroll
+            for (int i = 0; i < PPW; ++i)
+                j.x[s][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(span_of(p.sh_acc), from0 + part * step + (pc + i) * 1024, 0, kDeviceScope));
+        }
+        float top = M;
+#pragma unroll
+        for (int s = 0; s < N; ++s) top = fmaxf(top, __uint_as_float(j.head[s][0])); // (the own part counts twice at most)
+        const float f = __builtin_amdgcn_exp2f(M - top);
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < PPW; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[i][e] *= f;
+        M = top;
+        join_parts(all, s0, pc, j, M, l, o);
+    }
+    if (active) {
+        const int b = row / p.rows, r = row - b * p.rows;
+        const float inv = 1.f / l;
+        uint16_t* to = (uint16_t*)p.out + row_offset(p, b, kvh, r, row_node(p, r)) + pc * 16 + 4 * half;
+#pragma unroll
+        for (int i = 0; i < PPW; ++i) {
+            *(u32x2*)(to + i * 16) = pack_partial(o[i][0], o[i][1], o[i][2], o[i][3], inv);
+            *(u32x2*)(to + i * 16 + 8) = pack_partial(o[i][4], o[i][5], o[i][6], o[i][7], inv);
+        }
+    }
+}
+
 // Statuses, by workgroups of their own behind the last one of the launch over the sequences' own keys, a wave a sequence: the trips of a report in a row, up
 // to the block ids, would otherwise be a tail of the workgroups that also compute. `first`: the first such workgroup's number.
-__device__ __forceinline__ void report_shared(const SharedParams& p, int first) {
-    const int lane = threadIdx.x & 63, b = ((int)blockIdx.x - first) * ((int)blockDim.x >> 6) + ((int)threadIdx.x >> 6);
+__device__ __forceinline__ void report_shared(const SharedParams& p, uint32_t first) {
+    const int lane = threadIdx.x & 63, b = (int)(blockIdx.x - first) * ((int)blockDim.x >> 6) + ((int)threadIdx.x >> 6);
     if (!p.status || b >= p.B) return;
     const int32_t parent = p.parent[(int64_t)b * p.T + min(lane, p.T - 1)], S = p.prefix_len[b], len = p.shared_len[0];
     bool bad = false;

@@ -85,12 +85,14 @@ struct AttnParams {
 
 // Attention of a batch behind one shared prefix, in two launches: all sequences' rows against the shared keys, whose partial results stay
 // in fp32, and every sequence's rows against its own keys, joined with them.
-enum RowsMode { kRowsWhole = 0, kRowsShared = 1, kRowsOwn = 2 }; // the kernels of vs_tree_verify_attention, and these two
+enum RowsMode { kRowsWhole = 0, kRowsShared = 1, kRowsOwn = 2, kRowsBoth = 3 }; // the kernels of vs_tree_verify_attention; these two; both in one launch
 struct SharedParams : AttnParams {
     float* sh_acc;              // the parts' means (bf16 storage) or sums of weights times values, see attn_shared.h
     float* sh_ml;               // [KV head][part][row]: reference (log2 domain), sum of weights; bf16 storage: and exponents
+    uint64_t* sh_words;         // one launch for both: a word per (sequence, KV head)
     const int32_t* shared_len;
     const int32_t* shared_table; // paged only
+    int32_t sh_batch, sh_own_rows; // sequences, and rows of one
     int32_t sh_rows, sh_blocks; // rows of all sequences, B * T * group, and 32-row blocks of them
     int32_t sh_splits, sh_keys_per_split; // places for parts of a row, at most; keys of one where the parts are equal splits
     int32_t sh_shares;          // else the number of shares of all (KV head, row group) units' keys, 0: equal splits
@@ -290,6 +292,7 @@ hipError_t launch_attention_mfma_resident(const AttnParams& p, int row_blocks, h
 hipError_t launch_attention_mfma_rows(const AttnParams& p, int waves, hipStream_t s);
 hipError_t launch_attention_mfma_rounds(const AttnParams& p, int row_blocks, hipStream_t s);
 hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, int waves, hipStream_t s);
+hipError_t launch_attention_shared_both(const SharedParams& shared, const SharedParams& own, hipStream_t s);
 hipError_t launch_attention_shared_pipe(const SharedParams& p, RowsMode mode, int waves, hipStream_t s);
 hipError_t launch_attention_shared_f32(const SharedParams& p, RowsMode mode, hipStream_t s);
 hipError_t launch_attention_combine(const AttnParams& p, int dtype, hipStream_t s);
