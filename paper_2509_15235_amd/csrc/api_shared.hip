@@ -1,5 +1,4 @@
 // C-ABI entry point of the attention behind a shared prefix: host-side checks, launch planning and enqueues.
-#include <stdlib.h>
 #include "vs_internal.h"
 
 namespace {
@@ -45,81 +44,137 @@ int32_t check_shared(const vs_attn_desc* d, const vs_prefix_desc* x, vs_attn_des
 struct Cut {
     int32_t rows_per_group, row_groups, num_splits, keys_per_split, total_wgs;
 };
+// How the shared keys are worked on.
+enum Way : int32_t {
+    kWayAuto = 0,
+    kWayBoth8 = 1, // one launch with the sequences' own keys, workgroups of eight waves with key tiles of their own, one on a CU
+    kWayBoth4 = 2, // ... of four waves, two on a CU
+    kWayRows = 3,  // a launch of own tiles, equal splits
+    kWayLine = 4,  // a launch of the pipelined kernel, all row groups' keys in one line of equal shares
+    kWayUnits = 5, // ... every row group's keys in the same number of shares
+    kWays = 6
+};
+thread_local int32_t asked_way = kWayAuto; // vs_internal_set_shared_way
 struct SharedPlan {
     Cut shared, own;
-    int32_t own_waves, own_pipe;
-    int32_t both;   // one launch
+    int32_t way, own_waves, own_pipe;
     int32_t places; // for parts of a row
-    int32_t steps, longer, per_line, line_steps; // of a share, of a line of shares
-    int32_t waves, shares; // the pipelined kernel on equal shares of all row groups' keys; 0: own tiles, equal splits
+    int32_t shares, steps, longer, per_line, line_steps; // (kWayLine, kWayUnits) all, steps of one, how many have one more, shares and steps of a line
+    float cost;
     size_t acc_bytes, ml_bytes, word_bytes;
 };
+struct SharedSize {
+    int64_t rows, own_rows, own_units; // of a KV head; of a sequence's; (sequence, KV head)s
+    int32_t B, Hkv, d, tiles;          // tiles of 64 keys
+    bool f32, same_paging;
+};
+
+// Equal splits for kernels with tiles of a wave's own, `waves` waves to a workgroup: places / workgroups of them, at most `most`, of four tiles or more.
+bool cut_rows(const SharedSize& z, int32_t rows_per_group, int64_t places, int32_t most, Cut& s) {
+    s.rows_per_group = rows_per_group;
+    s.row_groups = (int32_t)((z.rows + rows_per_group - 1) / rows_per_group);
+    const int64_t wgs = (int64_t)z.Hkv * s.row_groups;
+    int64_t splits = places / wgs;
+    if (splits > (z.tiles + 3) / 4) splits = (z.tiles + 3) / 4;
+    if (splits > most) splits = most;
+    if (splits < 1) splits = 1;
+    const int tps = (int)((z.tiles + splits - 1) / splits);
+    s.keys_per_split = tps * kIterKeys;
+    s.num_splits = (z.tiles + tps - 1) / tps;
+    s.total_wgs = (int32_t)(wgs * s.num_splits);
+    return wgs <= places;
+}
+// 32-key tiles that a wave of such a launch takes one after the other
+int64_t wave_tiles(const Cut& s, int32_t waves) { return (s.keys_per_split / kTileKeys + waves - 1) / waves; }
+
+// One way's plan with its cost, the call's us as a straight line through what was measured; false: not for this call.
+// us per call, 28 / 4 heads of 128 channels and paged caches unless stated, up to 200 own keys, by way Both8 / Both4 / Rows / Line or Units:
+//   4 x 1 token, 1696 keys 10.0 / - / 13.5 / -; 8192 keys 13.5 / - / 20.1 / -; 20 x 1, 600 keys 12.5 / - / - / 21.4, 8192 keys 21.8 / - / - / 25.9
+//   30 x 4, 8192 keys 52 / - / - / 37; 60 x 4, 8 / 1 heads, 8192 keys 23.4 / - / - / 31.9
+//   64 x 1, 600 keys - / 13.8 / 18.0 / 23.2, 1696 keys - / 18.2 / 19.0 / 23.8, 8192 keys - / 31.2 / 30.1 / 33.9; 80 x 1, 8192 keys - / 44.8 / 29.9 / 35.6
+//   64 x 4, 600 keys - / 18.1 / 20.5 / 24.8, 1696 keys - / 26.9 / 24.7 / 27.6, 8192 keys - / 78.6 / 54.8 / 51.7
+//   10 x 1, 32 / 32 heads, 4096 keys - / 20.6 / 24.9 / -; 14 x 1 - / 26.5 / 25.5 / -; 40 x 1, 32 / 8 heads of 64, 8192 keys 15.7 / 21.2 / 19.1 / 27.5
+bool plan_way(const SharedSize& z, int32_t way, SharedPlan& pl) {
+    pl = SharedPlan{};
+    pl.way = way;
+    Cut& s = pl.shared;
+    if (way == kWayBoth8 || way == kWayBoth4) {
+        const int32_t waves = way == kWayBoth8 ? 8 : 4;
+        // Parts beyond fifteen, with the own one, take the join a third trip to memory: 4 x 1, 8192 keys in 32 / 16 splits 15.5 / 13.5.
+        if (z.f32 || z.own_rows > kRowBlock || !z.same_paging) return false;
+        const int64_t places = (way == kWayBoth8 ? 1 : 2) * kNumCUs - z.own_units;
+        if (places < 1 || !cut_rows(z, kRowBlock, places, 15, s)) return false;
+        pl.cost = (waves == 8 ? 8.5f + 1.35f * wave_tiles(s, 8) : 12.f + 1.2f * wave_tiles(s, 4)) + 0.2f * s.num_splits;
+        return true;
+    }
+    if (way == kWayRows) {
+        const bool two = z.d == 128 && z.rows > kRowBlock;
+        cut_rows(z, z.f32 ? 8 : two ? 2 * kRowBlock : kRowBlock, kNumCUs, kMergeMaxSplits, s);
+        const float rounds = (float)((s.total_wgs + kNumCUs - 1) / kNumCUs);
+        pl.cost = 15.5f + (two ? 2.5f : 1.35f) * wave_tiles(s, 8) * rounds + 0.3f * s.num_splits;
+        return true;
+    }
+    if (z.f32 || z.rows <= kRowBlock) return false;
+    s.rows_per_group = 8 * kRowBlock;
+    s.row_groups = (int32_t)((z.rows + s.rows_per_group - 1) / s.rows_per_group);
+    const int64_t units = (int64_t)z.Hkv * s.row_groups, steps = units * z.tiles;
+    if (steps > 0x7fffffff) return false;
+    int64_t shares, per, line;
+    if (way == kWayLine) { // the CUs end together, but a share that ends one row group and begins another pays twice for a beginning and an end
+        shares = per = steps / 4 < kNumCUs ? (steps + 3) / 4 : kNumCUs;
+        line = steps;
+    } else {
+        per = kNumCUs / units;
+        if (per > z.tiles / 4) per = z.tiles / 4;
+        if (per < 1) per = 1;
+        shares = units * per;
+        line = z.tiles;
+    }
+    pl.shares = (int32_t)shares;
+    pl.per_line = (int32_t)per;
+    pl.line_steps = (int32_t)line;
+    pl.steps = (int32_t)(line / per);
+    pl.longer = (int32_t)(line % per);
+    // a row group's steps begin in one share and end in another: at most so many
+    s.num_splits = way == kWayUnits ? (int32_t)per : (int32_t)((z.tiles + pl.steps - 1) / pl.steps) + 1;
+    s.keys_per_split = kIterKeys;
+    s.total_wgs = pl.shares;
+    const float rounds = (float)((shares + kNumCUs - 1) / kNumCUs);
+    pl.cost = 15.5f + rounds * 2.3f * (float)((line + per - 1) / per) + (way == kWayLine ? 9.f : 0.f) + 0.3f * s.num_splits;
+    return true;
+}
 
 SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
-    SharedPlan pl{};
     const int group = d->Hq / d->Hkv;
-    const int64_t rows = (int64_t)d->B * d->T * group;
     const bool f32 = d->dtype == VS_F32;
-    const int tiles = (prefix.max_prefix_len + kIterKeys - 1) / kIterKeys;
-    Cut& s = pl.shared;
-    if (!f32 && (int64_t)d->Hkv * ((rows + 255) / 256) * tiles <= 0x7fffffff && rows > (getenv("PIPEROWS") ? atoi(getenv("PIPEROWS")) : 128)) {
-        pl.waves = getenv("W4") ? 4 : 8;
-        s.rows_per_group = pl.waves * kRowBlock;
-        s.row_groups = (int32_t)((rows + s.rows_per_group - 1) / s.rows_per_group);
-        const int64_t units = (int64_t)d->Hkv * s.row_groups, steps = units * tiles, places = kNumCUs * (pl.waves == 8 ? 1 : 2);
-        // Shares anywhere: all CUs end together, but a share that ends one unit and begins another pays for two beginnings and ends, 8 steps' time or so each.
-        // Or every unit in the same number of them.
-        int64_t shares = steps / 4 < places ? (steps + 3) / 4 : places, whole = places / units;
-        if (whole > tiles / 4) whole = tiles / 4;
-        if (whole < 1) whole = 1;
-        const int64_t any = (steps + shares - 1) / shares + 9, even = ((tiles + whole - 1) / whole + 4) * ((units * whole + places - 1) / places);
-        const bool lines = even <= any;
-        const int64_t per = lines ? whole : shares, line = lines ? tiles : steps;
-        pl.shares = (int32_t)(lines ? units * whole : shares);
-        pl.per_line = (int32_t)per;
-        pl.line_steps = (int32_t)line;
-        pl.steps = (int32_t)(line / per);
-        pl.longer = (int32_t)(line % per);
-        // a unit's steps begin in one share and end in another: at most so many
-        s.num_splits = lines ? (int32_t)whole : (int32_t)((tiles + pl.steps - 1) / pl.steps) + 1;
-        s.keys_per_split = kIterKeys;
-        s.total_wgs = pl.shares;
-    } else {
-        // One launch for both kinds of work where all workgroups run at once (and one row block of the shared keys to a workgroup): us per call,
-        // two launches / one
-        const int64_t blocks = (rows + kRowBlock - 1) / kRowBlock, own = (int64_t)d->B * d->Hkv;
-        pl.both = !f32 && d->T * group <= kRowBlock && (d->paged != 0) == (prefix.paged != 0) && own + blocks * d->Hkv <= kNumCUs && !getenv("NOBOTH");
-        s.rows_per_group = f32 ? 8 : d->d == 128 && rows > kRowBlock && !pl.both ? 2 * kRowBlock : kRowBlock;
-        s.row_groups = (int32_t)((rows + s.rows_per_group - 1) / s.rows_per_group);
-        const int64_t wgs = (int64_t)d->Hkv * s.row_groups;
-        int64_t splits = (kNumCUs - (pl.both ? own : 0)) / wgs;
-        if (splits > (tiles + 3) / 4) splits = (tiles + 3) / 4;
-        if (splits > kMergeMaxSplits) splits = kMergeMaxSplits;
-        if (splits < 1) splits = 1;
-        const int tps = (int)((tiles + splits - 1) / splits);
-        s.keys_per_split = tps * kIterKeys;
-        s.num_splits = (tiles + tps - 1) / tps;
-        s.total_wgs = (int32_t)(wgs * s.num_splits);
+    const SharedSize z{(int64_t)d->B * d->T * group, d->T * group, (int64_t)d->B * d->Hkv, d->B, d->Hkv, d->d, (prefix.max_prefix_len + kIterKeys - 1) / kIterKeys,
+                       f32, (d->paged != 0) == (prefix.paged != 0)};
+    SharedPlan pl{};
+    if (asked_way == kWayAuto || !plan_way(z, asked_way, pl)) {
+        plan_way(z, kWayRows, pl);
+        for (int32_t way = kWayAuto + 1; way < kWays; ++way) {
+            SharedPlan other;
+            if (plan_way(z, way, other) && other.cost < pl.cost) pl = other;
+        }
     }
+    const bool both = pl.way == kWayBoth8 || pl.way == kWayBoth4;
     Cut& o = pl.own;
     const int own_rows = d->T * group;
-    o.rows_per_group = f32 ? ((int64_t)d->B * d->Hkv * ((own_rows + 3) / 4) <= kNumCUs ? 4 : 8) : d->d == 128 && own_rows > kRowBlock ? 2 * kRowBlock : kRowBlock;
-    if (!f32 && own_rows > 2 * kRowBlock) {
-        pl.own_pipe = 1;
-        pl.own_waves = getenv("OWN8") ? 8 : 4;
-        o.rows_per_group = pl.own_waves * kRowBlock;
-    }
+    pl.own_pipe = !f32 && own_rows > 2 * kRowBlock;
+    o.rows_per_group = f32 ? (z.own_units * ((own_rows + 3) / 4) <= kNumCUs ? 4 : 8) : pl.own_pipe ? 4 * kRowBlock : d->d == 128 && own_rows > kRowBlock ? 2 * kRowBlock : kRowBlock;
     o.row_groups = (own_rows + o.rows_per_group - 1) / o.rows_per_group;
     o.num_splits = 1;
     o.keys_per_split = (int32_t)(((int64_t)d->max_prefix_len + d->T + kIterKeys - 1) / kIterKeys * kIterKeys);
     o.total_wgs = d->B * d->Hkv * o.row_groups;
-    if (!pl.own_pipe) pl.own_waves = o.rows_per_group > kRowBlock || o.total_wgs <= kNumCUs ? 8 : d->d == 64 ? 2 : 4;
-    pl.places = s.num_splits + (pl.both ? 1 : 0);
+    // More workgroups than CUs: short ones of fewer waves, several to a CU. us per call, 32 x 1 token of 32 / 32 heads behind 4099 keys, eight waves / four / two
+    // 63 / 44.4 / 46.7, 200 .. 1000 own keys - / 79 / 85; 64 x 1 of 16 / 16 heads of 64 - / 21.6 / 19.4.
+    pl.own_waves = pl.own_pipe ? 4 : o.rows_per_group > kRowBlock || o.total_wgs <= kNumCUs ? 8 : d->d == 64 ? 2 : 4;
+    pl.places = pl.shared.num_splits + (both ? 1 : 0);
     const size_t parts = (size_t)d->Hkv * pl.places;
-    const size_t padded = (rows + kRowBlock - 1) / kRowBlock * kRowBlock; // whole row blocks
-    pl.acc_bytes = align_up(parts * (f32 ? rows * d->d * sizeof(float) : padded * d->d * sizeof(uint16_t)));
-    pl.ml_bytes = align_up(parts * rows * (f32 ? 2 : 4) * sizeof(float));
-    if (pl.both) pl.word_bytes = (size_t)d->B * d->Hkv * kArrivalWords * sizeof(uint64_t);
+    const size_t padded = (z.rows + kRowBlock - 1) / kRowBlock * kRowBlock; // whole row blocks
+    pl.acc_bytes = align_up(parts * (f32 ? z.rows * d->d * sizeof(float) : padded * d->d * sizeof(uint16_t)));
+    pl.ml_bytes = align_up(parts * z.rows * (f32 ? 2 : 4) * sizeof(float));
+    if (both) pl.word_bytes = (size_t)z.own_units * kArrivalWords * sizeof(uint64_t);
     return pl;
 }
 
@@ -169,6 +224,13 @@ SharedParams shared_params(const AttnParams& base, const Cut& c, const SharedPla
 
 extern "C" {
 
+void vs_internal_set_shared_way(int32_t way) { asked_way = way; }
+int32_t vs_internal_shared_way(const vs_attn_desc* desc, const vs_prefix_desc* prefix) {
+    vs_attn_desc x;
+    const int32_t rc = check_shared(desc, prefix, x);
+    return rc != VS_OK ? rc : plan_shared(desc, x).way;
+}
+
 size_t vs_shared_prefix_workspace_bytes(const vs_attn_desc* desc, const vs_prefix_desc* prefix) {
     vs_attn_desc x;
     if (check_shared(desc, prefix, x) != VS_OK) return 0;
@@ -194,9 +256,18 @@ int32_t vs_shared_prefix_attention(const vs_attn_desc* desc, const vs_prefix_des
                                              shared_len, workspace);
     const SharedParams second = shared_params(attention_params(desc, 1, q, k_cache, v_cache, prefix_len, tree_parent, tree_mask, out, status), pl.own, pl, desc, x,
                                               shared_len, workspace);
-    if (pl.both) return launch_attention_shared_both(first, second, s) == hipSuccess ? VS_OK : VS_ERR_HIP;
-    hipError_t e = f32 ? launch_attention_shared_f32(first, kRowsShared, s) : pl.waves ? launch_attention_shared_pipe(first, kRowsShared, pl.waves, s) : launch_attention_shared_rows(first, kRowsShared, 8, s);
-    if (e == hipSuccess) e = f32 ? launch_attention_shared_f32(second, kRowsOwn, s) : pl.own_pipe ? launch_attention_shared_pipe(second, kRowsOwn, pl.own_waves, s) : launch_attention_shared_rows(second, kRowsOwn, pl.own_waves, s);
+    hipError_t e;
+    if (pl.way == kWayBoth8 || pl.way == kWayBoth4) {
+        e = launch_attention_shared_both(first, second, pl.way == kWayBoth8 ? 8 : 4, s);
+    } else {
+        e = f32 ? launch_attention_shared_f32(first, kRowsShared, s)
+            : pl.way == kWayRows ? launch_attention_shared_rows(first, kRowsShared, 8, s)
+                                 : launch_attention_shared_pipe(first, kRowsShared, 8, s);
+        if (e == hipSuccess)
+            e = f32 ? launch_attention_shared_f32(second, kRowsOwn, s)
+                : pl.own_pipe ? launch_attention_shared_pipe(second, kRowsOwn, pl.own_waves, s)
+                              : launch_attention_shared_rows(second, kRowsOwn, pl.own_waves, s);
+    }
     return e == hipSuccess ? VS_OK : VS_ERR_HIP;
 }
 

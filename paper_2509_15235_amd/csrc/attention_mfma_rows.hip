@@ -524,12 +524,11 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const RowsAr
         __syncthreads();
         const uint32_t todo = (uint32_t)sflag;
         if (todo == 0) return;
-        // 32 rows at a time: of this row block, and what its first and last sequence have in the ones beside it
         const int first_b = shared_work ? row0 / p.sh_own_rows : b;
         const int from = (first_b + __builtin_ctz(todo)) * p.sh_own_rows, to = (first_b + 32 - __builtin_clz(todo)) * p.sh_own_rows;
-        for (int at = shared_work ? from / kRowBlock * kRowBlock : from; at < to; at += kRowBlock) {
+        for (int at = from; at < to; at += kRowBlock) {
             const int row = at + col, which = row / p.sh_own_rows - first_b;
-            join_rows<D, NW>(args.work[0], kvh, live, row, row >= from && row < to && ((todo >> which) & 1) != 0);
+            join_rows<D, NW>(args.work[0], kvh, live, row, row < to && ((todo >> which) & 1) != 0);
         }
     }
     if constexpr (MODE == kRowsWhole)
@@ -577,11 +576,12 @@ hipError_t launch_both(const BothParams& p, hipStream_t s) {
 }
 } // namespace
 
-hipError_t launch_attention_shared_both(const SharedParams& shared, const SharedParams& own, hipStream_t s) {
+hipError_t launch_attention_shared_both(const SharedParams& shared, const SharedParams& own, int waves, hipStream_t s) {
     if (shared.rows_per_group != kRowBlock || own.rows > kRowBlock || own.row_groups != 1 || own.num_splits != 1 || shared.paged != own.paged) return hipErrorInvalidValue;
-    if ((own.d != 64 && own.d != 128) || shared.sh_splits != shared.num_splits + 1) return hipErrorInvalidValue;
+    if ((waves != 4 && waves != 8) || (own.d != 64 && own.d != 128) || shared.sh_splits != shared.num_splits + 1) return hipErrorInvalidValue;
     const BothParams p{{own, shared}};
-    return own.d == 128 ? launch_both<128, 8>(p, s) : launch_both<64, 8>(p, s);
+    if (own.d == 128) return waves == 8 ? launch_both<128, 8>(p, s) : launch_both<128, 4>(p, s);
+    return waves == 8 ? launch_both<64, 8>(p, s) : launch_both<64, 4>(p, s);
 }
 
 hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, int waves, hipStream_t s) {

@@ -272,6 +272,11 @@ extern "C" int32_t vs_internal_reads_once(const vs_attn_desc* desc, int32_t tree
 
 inline bool is_pow2(int32_t x) { return x > 0 && (x & (x - 1)) == 0; }
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+// How vs_shared_prefix_attention works on the shared keys, in the calling thread's next calls (1 .. 5, see api_shared.hip; 0, or one that is not for a call:
+// the cheapest), and what a call with these descriptors takes (or a vs_error): for tests. A workspace is sized for the way asked for then.
+extern "C" void vs_internal_set_shared_way(int32_t way);
+extern "C" int32_t vs_internal_shared_way(const vs_attn_desc* desc, const vs_prefix_desc* prefix);
+
 int32_t check_attention(const vs_attn_desc* d, int tree); // shapes, types and layouts that need no device (api.hip)
 // What a descriptor says, as the kernels take it; the plan's numbers are left at zero (api.hip)
 AttnParams attention_params(const vs_attn_desc* d, int tree, const void* q, const void* k_cache, const void* v_cache, const int32_t* prefix_len,
@@ -292,7 +297,7 @@ hipError_t launch_attention_mfma_resident(const AttnParams& p, int row_blocks, h
 hipError_t launch_attention_mfma_rows(const AttnParams& p, int waves, hipStream_t s);
 hipError_t launch_attention_mfma_rounds(const AttnParams& p, int row_blocks, hipStream_t s);
 hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, int waves, hipStream_t s);
-hipError_t launch_attention_shared_both(const SharedParams& shared, const SharedParams& own, hipStream_t s);
+hipError_t launch_attention_shared_both(const SharedParams& shared, const SharedParams& own, int waves, hipStream_t s);
 hipError_t launch_attention_shared_pipe(const SharedParams& p, RowsMode mode, int waves, hipStream_t s);
 hipError_t launch_attention_shared_f32(const SharedParams& p, RowsMode mode, hipStream_t s);
 hipError_t launch_attention_combine(const AttnParams& p, int dtype, hipStream_t s);
