@@ -160,15 +160,19 @@ SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
     const bool both = pl.way == kWayBoth8 || pl.way == kWayBoth4;
     Cut& o = pl.own;
     const int own_rows = d->T * group;
-    pl.own_pipe = !f32 && own_rows > 2 * kRowBlock;
-    o.rows_per_group = f32 ? (z.own_units * ((own_rows + 3) / 4) <= kNumCUs ? 4 : 8) : pl.own_pipe ? 4 * kRowBlock : d->d == 128 && own_rows > kRowBlock ? 2 * kRowBlock : kRowBlock;
+    // A workgroup for every row block, whose waves share the keys out; four of them together in the pipelined kernel where that would be many rounds of workgroups. us per
+    // call behind 600 keys, 28 / 4 heads, 20 / 200 / 700 own keys at most, row blocks / pipelined:
+    //   8 x 10 nodes 15.9 17.0 19.3 / 18.2 22.4 32.2; 16 x 30 21.2 23.0 28.6 / 24.8 29.7 39.0; 16 x 60 33.8 35.9 45.2 / 32.5 36.1 46.5; 32 x 60 53.8 56.4 70.7 / 46.3 50.7 66.4
+    // (Two row blocks to a workgroup lose to both: 8 x 10 19.8 20.6 24.2.)
+    pl.own_pipe = !f32 && own_rows > 2 * kRowBlock && z.own_units * ((own_rows + kRowBlock - 1) / kRowBlock) > 4 * kNumCUs;
+    o.rows_per_group = f32 ? (z.own_units * ((own_rows + 3) / 4) <= kNumCUs ? 4 : 8) : pl.own_pipe ? 4 * kRowBlock : kRowBlock;
     o.row_groups = (own_rows + o.rows_per_group - 1) / o.rows_per_group;
     o.num_splits = 1;
     o.keys_per_split = (int32_t)(((int64_t)d->max_prefix_len + d->T + kIterKeys - 1) / kIterKeys * kIterKeys);
     o.total_wgs = d->B * d->Hkv * o.row_groups;
     // More workgroups than CUs: short ones of fewer waves, several to a CU. us per call, 32 x 1 token of 32 / 32 heads behind 4099 keys, eight waves / four / two
     // 63 / 44.4 / 46.7, 200 .. 1000 own keys - / 79 / 85; 64 x 1 of 16 / 16 heads of 64 - / 21.6 / 19.4.
-    pl.own_waves = pl.own_pipe ? 4 : o.rows_per_group > kRowBlock || o.total_wgs <= kNumCUs ? 8 : d->d == 64 ? 2 : 4;
+    pl.own_waves = pl.own_pipe ? 4 : o.total_wgs <= kNumCUs ? 8 : d->d == 64 ? 2 : 4;
     pl.places = pl.shared.num_splits + (both ? 1 : 0);
     const size_t parts = (size_t)d->Hkv * pl.places;
     const size_t padded = (z.rows + kRowBlock - 1) / kRowBlock * kRowBlock; // whole row blocks
@@ -262,10 +266,10 @@ int32_t vs_shared_prefix_attention(const vs_attn_desc* desc, const vs_prefix_des
     } else {
         e = f32 ? launch_attention_shared_f32(first, kRowsShared, s)
             : pl.way == kWayRows ? launch_attention_shared_rows(first, kRowsShared, 8, s)
-                                 : launch_attention_shared_pipe(first, kRowsShared, 8, s);
+                                 : launch_attention_shared_pipe(first, kRowsShared, s);
         if (e == hipSuccess)
             e = f32 ? launch_attention_shared_f32(second, kRowsOwn, s)
-                : pl.own_pipe ? launch_attention_shared_pipe(second, kRowsOwn, pl.own_waves, s)
+                : pl.own_pipe ? launch_attention_shared_pipe(second, kRowsOwn, s)
                               : launch_attention_shared_rows(second, kRowsOwn, pl.own_waves, s);
     }
     return e == hipSuccess ? VS_OK : VS_ERR_HIP;

@@ -1153,17 +1153,14 @@ hipError_t launch_pipe_shared(const SharedParams& p, hipStream_t s) {
     else hipLaunchKernelGGL((attn_mfma_pipe_kernel<D, 1, NW, false, false, false, MODE>), grid, block, 0, s, p);
     return hipGetLastError();
 }
-template <int MODE>
-hipError_t launch_pipe_shared(const SharedParams& p, int waves, hipStream_t s) {
-    if (p.d == 128) return waves == 8 ? launch_pipe_shared<128, 8, MODE>(p, s) : launch_pipe_shared<128, 4, MODE>(p, s);
-    return waves == 8 ? launch_pipe_shared<64, 8, MODE>(p, s) : launch_pipe_shared<64, 4, MODE>(p, s);
-}
 } // namespace
 
-hipError_t launch_attention_shared_pipe(const SharedParams& p, RowsMode mode, int waves, hipStream_t s) {
-    if ((waves != 4 && waves != 8) || p.rows_per_group != waves * kRowBlock || (p.d != 128 && p.d != 64)) return hipErrorInvalidValue;
+// The shared keys with eight waves to a workgroup, the sequences' own with four.
+hipError_t launch_attention_shared_pipe(const SharedParams& p, RowsMode mode, hipStream_t s) {
+    if (p.rows_per_group != (mode == kRowsShared ? 8 : 4) * kRowBlock || (p.d != 128 && p.d != 64)) return hipErrorInvalidValue;
     if (mode == kRowsShared ? p.sh_shares < 1 : p.num_splits != 1 || p.row_groups * p.rows_per_group < p.rows) return hipErrorInvalidValue;
-    return mode == kRowsShared ? launch_pipe_shared<kRowsShared>(p, waves, s) : launch_pipe_shared<kRowsOwn>(p, waves, s);
+    if (mode == kRowsShared) return p.d == 128 ? launch_pipe_shared<128, 8, kRowsShared>(p, s) : launch_pipe_shared<64, 8, kRowsShared>(p, s);
+    return p.d == 128 ? launch_pipe_shared<128, 4, kRowsOwn>(p, s) : launch_pipe_shared<64, 4, kRowsOwn>(p, s);
 }
 
 // One row block per wave; four waves (two workgroups per CU) or eight.

@@ -199,8 +199,9 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const RowsAr
     // kRowsOwn: this wave's pieces of the first parts against the shared keys
     constexpr int PPW = NP / NW > 0 ? NP / NW : 1;
     constexpr int EARLY = MODE == kRowsOwn ? (PPW == 1 ? 8 : 4) : 1;
-    JoinParts<EARLY, PPW> parts; // (two row blocks have no registers for them yet)
-    SharedRow joined[MODE == kRowsOwn ? RB : 1];
+    JoinParts<EARLY, PPW> parts;
+    SharedRow joined;
+    static_assert(MODE != kRowsOwn || RB == 1, "one row block");
     const int my_piece = min(wave, NP / PPW - 1) * PPW;
     // kRowsBoth: how many parts of the shared keys there are; wave 0: the sequence whose word the lane arrives at, and what that holds
     int live = 0, to_b = -1;
@@ -215,12 +216,8 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const RowsAr
         }
         live = shared_parts(p, p.shared_len[0], kvh, 0);
     } else if constexpr (MODE == kRowsOwn) {
-        const int32_t shared = p.shared_len[0];
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            joined[rb] = shared_at<D>(p, shared, kvh, b * p.rows + min(row0 + rb * kRowBlock + col, p.rows - 1), half);
-        }
-        if constexpr (RB == 1) load_parts(joined[0], 0, my_piece, parts);
+        joined = shared_at<D>(p, p.shared_len[0], kvh, b * p.rows + min(row0 + col, p.rows - 1), half);
+        load_parts(joined, 0, my_piece, parts);
     }
     if (first < kend) { // uniform per wave
         issue(std::false_type{}, sK, first, kend - 1);
@@ -476,8 +473,7 @@ __global__ __launch_bounds__(NW * 64, 2) void attn_mfma_rows_kernel(const RowsAr
                     continue;
                 } else {
                     float sum = l;
-                    if constexpr (RB > 1) load_parts(joined[rb], 0, my_piece, parts);
-                    join_row(joined[rb], my_piece, parts, M, sum, r);
+                    join_row(joined, my_piece, parts, M, sum, r);
                     inv = 1.f / sum;
                 }
             }
@@ -559,8 +555,9 @@ hipError_t launch_shared(const SharedParams& p, hipStream_t s) {
     return hipGetLastError();
 }
 template <int D>
-hipError_t launch_shared_own(const SharedParams& p, int waves, hipStream_t s) {
-    return waves == 8 ? launch_shared<D, 8, 1, kRowsOwn>(p, s) : waves == 4 ? launch_shared<D, 4, 1, kRowsOwn>(p, s) : launch_shared<D, 2, 1, kRowsOwn>(p, s);
+hipError_t launch_shared_own(const SharedParams& p, int waves, hipStream_t s) { // eight waves, or four (64 channels: two)
+    constexpr int FEW = D == 128 ? 4 : 2;
+    return waves == 8 ? launch_shared<D, 8, 1, kRowsOwn>(p, s) : waves == FEW ? launch_shared<D, FEW, 1, kRowsOwn>(p, s) : hipErrorInvalidValue;
 }
 
 } // namespace
@@ -588,9 +585,9 @@ hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, in
     const int blocks = p.rows_per_group / kRowBlock;
     if (p.row_groups * p.rows_per_group < p.rows || (p.d != 64 && p.d != 128) || blocks < 1 || blocks > (p.d == 128 ? 2 : 1)) return hipErrorInvalidValue;
     if (p.keys_per_split % kIterKeys || (mode == kRowsOwn && p.num_splits != 1)) return hipErrorInvalidValue;
-    if (mode == kRowsOwn && blocks == 1) return p.d == 128 ? launch_shared_own<128>(p, waves, s) : launch_shared_own<64>(p, waves, s);
+    if (mode == kRowsOwn && blocks != 1) return hipErrorInvalidValue;
+    if (mode == kRowsOwn) return p.d == 128 ? launch_shared_own<128>(p, waves, s) : launch_shared_own<64>(p, waves, s);
     if (waves != 8) return hipErrorInvalidValue;
-    if (mode == kRowsOwn) return launch_shared<128, 8, 2, kRowsOwn>(p, s);
     if (p.d == 64) return launch_shared<64, 8, 1, kRowsShared>(p, s);
     return blocks == 2 ? launch_shared<128, 8, 2, kRowsShared>(p, s) : launch_shared<128, 8, 1, kRowsShared>(p, s);
 }

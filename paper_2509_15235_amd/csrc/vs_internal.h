@@ -298,7 +298,7 @@ hipError_t launch_attention_mfma_rows(const AttnParams& p, int waves, hipStream_
 hipError_t launch_attention_mfma_rounds(const AttnParams& p, int row_blocks, hipStream_t s);
 hipError_t launch_attention_shared_rows(const SharedParams& p, RowsMode mode, int waves, hipStream_t s);
 hipError_t launch_attention_shared_both(const SharedParams& shared, const SharedParams& own, int waves, hipStream_t s);
-hipError_t launch_attention_shared_pipe(const SharedParams& p, RowsMode mode, int waves, hipStream_t s);
+hipError_t launch_attention_shared_pipe(const SharedParams& p, RowsMode mode, hipStream_t s);
 hipError_t launch_attention_shared_f32(const SharedParams& p, RowsMode mode, hipStream_t s);
 hipError_t launch_attention_combine(const AttnParams& p, int dtype, hipStream_t s);
 hipError_t launch_accept(AcceptParams p, void* workspace, hipStream_t s);        // sets pairs, chunks
