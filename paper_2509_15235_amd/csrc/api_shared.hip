@@ -69,13 +69,13 @@ struct SharedSize {
     bool f32, same_paging;
 };
 
-// Equal splits for kernels with tiles of a wave's own, `waves` waves to a workgroup: places / workgroups of them, at most `most`, of four tiles or more.
-bool cut_rows(const SharedSize& z, int32_t rows_per_group, int64_t places, int32_t most, Cut& s) {
+// Equal splits: places / workgroups of them, at most `most`, of `least` tiles or more. Whether the workgroups fit the places.
+bool cut_rows(const SharedSize& z, int32_t rows_per_group, int64_t places, int32_t most, Cut& s, int32_t least = 4) {
     s.rows_per_group = rows_per_group;
     s.row_groups = (int32_t)((z.rows + rows_per_group - 1) / rows_per_group);
     const int64_t wgs = (int64_t)z.Hkv * s.row_groups;
     int64_t splits = places / wgs;
-    if (splits > (z.tiles + 3) / 4) splits = (z.tiles + 3) / 4;
+    if (splits > (z.tiles + least - 1) / least) splits = (z.tiles + least - 1) / least;
     if (splits > most) splits = most;
     if (splits < 1) splits = 1;
     const int tps = (int)((z.tiles + splits - 1) / splits);
@@ -109,7 +109,11 @@ bool plan_way(const SharedSize& z, int32_t way, SharedPlan& pl) {
     }
     if (way == kWayRows) {
         const bool two = z.d == 128 && z.rows > kRowBlock;
-        cut_rows(z, z.f32 ? 8 : two ? 2 * kRowBlock : kRowBlock, kNumCUs, kMergeMaxSplits, s);
+        // fp32: four rows to a workgroup, or eight, which share what is read, where four would fill the CUs without key splits; splits of two tiles or more. us per call,
+        // eight rows, splits of four / so: 6 x 5 nodes, 8 / 2 heads, 200, 601, 4000 keys 19.5 20.0 26.8 / 13.6 15.6 24.7; 16 x 1, 2000 keys 22.2 / 18.1; 4 x 2, 32 / 32
+        // heads, 4000 keys 41.5 / 36.4. (Always four: 16 x 8, 28 / 4 heads, 1100 keys 73.6 / 83.1; 8 x 4, 32 / 8 heads of 64, 2000 keys 19.4 / 21.2.)
+        if (z.f32) cut_rows(z, (int64_t)z.Hkv * ((z.rows + 3) / 4) * 128 <= (int64_t)kNumCUs * z.d ? 4 : 8, kNumCUs, kMergeMaxSplits, s, 2);
+        else cut_rows(z, two ? 2 * kRowBlock : kRowBlock, kNumCUs, kMergeMaxSplits, s);
         const float rounds = (float)((s.total_wgs + kNumCUs - 1) / kNumCUs);
         pl.cost = 15.5f + (two ? 2.5f : 1.35f) * wave_tiles(s, 8) * rounds + 0.3f * s.num_splits;
         return true;

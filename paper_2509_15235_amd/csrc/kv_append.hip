@@ -11,7 +11,7 @@ namespace vs {
 
 namespace {
 
-template <bool F32, bool HALVES, bool PAGED>
+template <bool F32, bool HALVES, bool PAGED, bool STREAM>
 __global__ __launch_bounds__(kRopeThreads) void kv_append_kernel(const AppendParams p) {
     __shared__ f32x2 cs[kRopeRows][kMaxRopePairs];
     __shared__ int64_t slot_at[kRopeRows]; // bytes from the caches' start to the row's slot of head 0; -1: none
@@ -108,8 +108,8 @@ __global__ __launch_bounds__(kRopeThreads) void kv_append_kernel(const AppendPar
                 if (slot_at[t] < 0) continue;
                 to = (head < p.Hq + p.Hkv ? (char*)p.k_cache + (head - p.Hq) * p.stride_head : (char*)p.v_cache + (head - p.Hq - p.Hkv) * p.stride_head) + slot_at[t];
             }
-            *(u32x4*)(to + piece * 16) = a[u];
-            if (HALVES && turns) *(u32x4*)(to + piece * 16 + p.rope.turning * 16) = b[u];
+            put<STREAM>(to + piece * 16, a[u]);
+            if (HALVES && turns) put<STREAM>(to + piece * 16 + p.rope.turning * 16, b[u]);
         }
         first += kRopeBatch * kRopeThreads;
         if (first - tid >= items) break;
@@ -136,19 +136,21 @@ __global__ __launch_bounds__(kRopeThreads) void kv_append_kernel(const AppendPar
     }
 }
 
-template <bool F32, bool HALVES>
-void launch_paged(const AppendParams& p, dim3 grid, hipStream_t s) {
-    if (p.paged) hipLaunchKernelGGL((kv_append_kernel<F32, HALVES, true>), grid, dim3(kRopeThreads), 0, s, p);
-    else hipLaunchKernelGGL((kv_append_kernel<F32, HALVES, false>), grid, dim3(kRopeThreads), 0, s, p);
+template <bool F32, bool HALVES, bool STREAM>
+void launch(const AppendParams& p, dim3 grid, hipStream_t s) {
+    if (p.paged) hipLaunchKernelGGL((kv_append_kernel<F32, HALVES, true, STREAM>), grid, dim3(kRopeThreads), 0, s, p);
+    else hipLaunchKernelGGL((kv_append_kernel<F32, HALVES, false, STREAM>), grid, dim3(kRopeThreads), 0, s, p);
 }
+template <bool F32, bool HALVES>
+void launch(const AppendParams& p, dim3 grid, hipStream_t s) { p.stream_out ? launch<F32, HALVES, true>(p, grid, s) : launch<F32, HALVES, false>(p, grid, s); }
 
 } // namespace
 
 hipError_t launch_kv_append(const AppendParams& p, int dtype, bool halves, hipStream_t s) {
     const int all_heads = p.Hq + 2 * p.Hkv;
     const dim3 grid((unsigned)((p.rows + p.rows_per_wg - 1) / p.rows_per_wg), (unsigned)((all_heads + p.heads_per_wg - 1) / p.heads_per_wg));
-    if (dtype == VS_F32) halves ? launch_paged<true, true>(p, grid, s) : launch_paged<true, false>(p, grid, s);
-    else halves ? launch_paged<false, true>(p, grid, s) : launch_paged<false, false>(p, grid, s);
+    if (dtype == VS_F32) halves ? launch<true, true>(p, grid, s) : launch<true, false>(p, grid, s);
+    else halves ? launch<false, true>(p, grid, s) : launch<false, false>(p, grid, s);
     return hipGetLastError();
 }
 

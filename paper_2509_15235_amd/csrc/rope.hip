@@ -9,7 +9,7 @@ namespace vs {
 
 namespace {
 
-template <bool F32, bool HALVES>
+template <bool F32, bool HALVES, bool STREAM>
 __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeApplyParams p) {
     __shared__ f32x2 cs[kRopeRows][kMaxRopePairs];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -47,8 +47,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeApplyParam
             const int c = where[u] & 0xffff;
             const bool turns = c < p.rope.turning;
             if (turns) rope_turn<F32, HALVES>(a[u], b[u], cs[where[u] >> 16], c);
-            *(u32x4*)((char*)p.out + to[u]) = a[u];
-            if (HALVES && turns) *(u32x4*)((char*)p.out + to[u] + p.rope.turning * 16) = b[u];
+            put<STREAM>((char*)p.out + to[u], a[u]);
+            if (HALVES && turns) put<STREAM>((char*)p.out + to[u] + p.rope.turning * 16, b[u]);
         }
         first += kRopeBatch * kRopeThreads;
         if (first - tid >= items) break;
@@ -56,18 +56,18 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(const RopeApplyParam
     }
 }
 
+template <bool F32, bool HALVES>
+void launch(const RopeApplyParams& p, dim3 grid, hipStream_t s) {
+    if (p.stream_out) hipLaunchKernelGGL((rope_kernel<F32, HALVES, true>), grid, dim3(kRopeThreads), 0, s, p);
+    else hipLaunchKernelGGL((rope_kernel<F32, HALVES, false>), grid, dim3(kRopeThreads), 0, s, p);
+}
+
 } // namespace
 
 hipError_t launch_rope(const RopeApplyParams& p, int dtype, bool halves, hipStream_t s) {
     const dim3 grid((unsigned)((p.rows + p.rows_per_wg - 1) / p.rows_per_wg), (unsigned)((p.H + p.heads_per_wg - 1) / p.heads_per_wg));
-    const dim3 block(kRopeThreads);
-    if (dtype == VS_F32) {
-        if (halves) hipLaunchKernelGGL((rope_kernel<true, true>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((rope_kernel<true, false>), grid, block, 0, s, p);
-    } else {
-        if (halves) hipLaunchKernelGGL((rope_kernel<false, true>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((rope_kernel<false, false>), grid, block, 0, s, p);
-    }
+    if (dtype == VS_F32) halves ? launch<true, true>(p, grid, s) : launch<true, false>(p, grid, s);
+    else halves ? launch<false, true>(p, grid, s) : launch<false, false>(p, grid, s);
     return hipGetLastError();
 }
 

@@ -226,6 +226,7 @@ struct RopeApplyParams {
     int64_t x_row, x_head, out_row, out_head; // strides in bytes
     int32_t H;
     int32_t rows_per_wg, heads_per_wg;
+    int32_t stream_out;          // see streams_out() in api_append.hip
     FastDiv by_heads;            // heads_per_wg
     RopeParams rope;
 };
@@ -249,6 +250,7 @@ struct AppendParams {
     int32_t B, T, Hq, Hkv;
     int32_t row_bytes;           // of a head
     int32_t rows_per_wg, heads_per_wg;
+    int32_t stream_out;          // see streams_out() in api_append.hip
     int32_t paged, block_size, block_shift, max_blocks, num_blocks;
     FastDiv by_T, by_heads;      // T, heads_per_wg
     int64_t capacity;
