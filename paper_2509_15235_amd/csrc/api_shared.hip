@@ -8,6 +8,7 @@ using namespace vs;
 constexpr size_t kAlign = 256;
 inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 constexpr int64_t kMaxSharedRows = 1 << 20; // of a KV head: node_of_row_short() is exact up to 2^21, and a partial result of this many rows is 512 MB
+constexpr int32_t kMaxSharedLen = 1 << 30; // keys rounded up to whole tiles stay in 32 bits
 
 // The shared prefix as the cache of one sequence, all sequences' nodes its queries.
 vs_attn_desc prefix_as_desc(const vs_attn_desc* d, const vs_prefix_desc* x) {
@@ -34,6 +35,7 @@ int32_t check_shared(const vs_attn_desc* d, const vs_prefix_desc* x, vs_attn_des
         return VS_ERR_SHAPE;
     if (const int32_t rc = check_attention(d, 1)) return rc;
     if ((int64_t)d->B * d->T * (d->Hq / d->Hkv) > kMaxSharedRows) return VS_ERR_SHAPE;
+    if (x->max_len > kMaxSharedLen || d->max_prefix_len > kMaxSharedLen) return VS_ERR_SHAPE;
     prefix = prefix_as_desc(d, x);
     if (const int32_t rc = check_attention(&prefix, 0)) return rc;
     prefix.T = d->B * d->T;
@@ -186,6 +188,19 @@ SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
     return pl;
 }
 
+// Loads that leave nothing in the caches (nt) where one workgroup alone reads a tile, and there are `least` megabytes of K and V or more, up to the longest
+// allowed lengths: faster for who finds nothing there, as layers with caches of their own do. Only contiguous caches, without two rows in one place;
+// what several sequences read through their tables, they may find in the caches. us per call, 32 / 32 heads of 128 channels, over other data each
+// time (the same data), plain / the shared keys so / the own ones so:
+//   16 x 1 behind 8000 keys (131 MB; up to 300 own keys, 79 MB) 41.9 (35.8) / 37.8 (37.6) / 41.5 (37.0); 32 x 1 behind 4099 (67, 158 MB) 44.3 (37.8) / 41.2 (38.8) / 39.9 (39.4);
+//   up to 1000 own keys (525 MB) 79.1 (77.6) / 78.2 (73.2) / 71.3 (71.2); 64 x 1 behind 1000 (16, 315 MB) 54.3 (47.8) / 54.4 (47.7) / 50.7 (50.1);
+//   32 x 1 behind 500, up to 100 own keys (8, 53 MB) 22.9 (22.7) / 24.1 (24.0) / 23.9 (22.1); 64 x 1 of 16 / 16 heads of 64 behind 4099 (34, 79 MB) 19.7 (19.6) / 19.6 (19.5) / 20.8 (19.8)
+bool reads_once(const vs_attn_desc& d, int tree, const Cut& c, double least) {
+    const int64_t keys = (int64_t)d.max_prefix_len + (tree ? d.T : 0);
+    return !d.paged && c.row_groups == 1 && c.rows_per_group == kRowBlock && d.d == 128 && (double)d.B * d.Hkv * keys * d.d * 4e-6 >= least &&
+           rows_apart(d.d, keys, d.stride_tok, d.Hkv, d.stride_head, d.B, d.stride_seq);
+}
+
 SharedParams shared_params(const AttnParams& base, const Cut& c, const SharedPlan& pl, const vs_attn_desc* d, const vs_attn_desc& prefix, const int32_t* shared_len,
                            void* workspace) {
     SharedParams p{};
@@ -260,10 +275,14 @@ int32_t vs_shared_prefix_attention(const vs_attn_desc* desc, const vs_prefix_des
     if (const int32_t dc = check_device()) return dc;
     hipStream_t s = (hipStream_t)stream;
     const bool f32 = desc->dtype == VS_F32;
-    const SharedParams first = shared_params(attention_params(&x, 0, q, k_shared, v_shared, shared_len, nullptr, nullptr, nullptr, nullptr), pl.shared, pl, desc, x,
-                                             shared_len, workspace);
-    const SharedParams second = shared_params(attention_params(desc, 1, q, k_cache, v_cache, prefix_len, tree_parent, tree_mask, out, status), pl.own, pl, desc, x,
-                                              shared_len, workspace);
+    SharedParams first = shared_params(attention_params(&x, 0, q, k_shared, v_shared, shared_len, nullptr, nullptr, nullptr, nullptr), pl.shared, pl, desc, x,
+                                       shared_len, workspace);
+    SharedParams second = shared_params(attention_params(desc, 1, q, k_cache, v_cache, prefix_len, tree_parent, tree_mask, out, status), pl.own, pl, desc, x,
+                                        shared_len, workspace);
+    if (pl.way == kWayRows && !f32) {
+        first.once = reads_once(x, 0, pl.shared, 96.);
+        second.once = !pl.own_pipe && reads_once(*desc, 1, pl.own, 128.);
+    }
     hipError_t e;
     if (pl.way == kWayBoth8 || pl.way == kWayBoth4) {
         e = launch_attention_shared_both(first, second, pl.way == kWayBoth8 ? 8 : 4, s);

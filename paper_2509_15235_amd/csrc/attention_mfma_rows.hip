@@ -550,7 +550,11 @@ hipError_t launch_rows(const AttnParams& p, hipStream_t s) {
 template <int D, int NW, int RB, int MODE>
 hipError_t launch_shared(const SharedParams& p, hipStream_t s) {
     const dim3 grid(round_up8(p.total_wgs) + (MODE == kRowsOwn && p.status ? (p.B + NW - 1) / NW : 0)), block(NW * kWave);
-    if (p.paged) hipLaunchKernelGGL((attn_mfma_rows_kernel<D, NW, RB, true, false, false, MODE>), grid, block, 0, s, p);
+    if (p.once && p.paged) return hipErrorInvalidValue;
+    constexpr bool ONCE = D == 128 && RB == 1 && NW >= 4;
+    if (p.once && !ONCE) return hipErrorInvalidValue;
+    if (p.once) hipLaunchKernelGGL((attn_mfma_rows_kernel<D, NW, RB, false, ONCE, false, MODE>), grid, block, 0, s, p);
+    else if (p.paged) hipLaunchKernelGGL((attn_mfma_rows_kernel<D, NW, RB, true, false, false, MODE>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((attn_mfma_rows_kernel<D, NW, RB, false, false, false, MODE>), grid, block, 0, s, p);
     return hipGetLastError();
 }
