@@ -43,7 +43,8 @@ __device__ __forceinline__ void request_args(const T& p) {
     const uint32_t* w = (const uint32_t*)&p;
     constexpr int N = (sizeof(T) - 4) / 64;
     static_assert(N <= 7, "lines");
-    asm volatile("" ::"s"(w[0]), "s"(w[N > 0 ? 16 : 0]), "s"(w[N > 1 ? 32 : 0]), "s"(w[N > 2 ? 48 : 0]), "s"(w[N > 3 ? 64 : 0]), "s"(w[N > 4 ? 80 : 0]), "s"(w[N > 5 ? 96 : 0]), "s"(w[N > 6 ? 112 : 0]), "s"(w[sizeof(T) / 4 - 1]));
+    asm volatile("" ::"s"(w[0]), "s"(w[N > 0 ? 16 : 0]), "s"(w[N > 1 ? 32 : 0]), "s"(w[N > 2 ? 48 : 0]), "s"(w[N > 3 ? 64 : 0]), "s"(w[N > 4 ? 80 : 0]), "s"(w[sizeof(T) / 4 - 1]));
+    if constexpr (N > 5) asm volatile("" ::"s"(w[96]), "s"(w[N > 6 ? 112 : 96]));
 }
 
 // ---- Wave-wide reductions on the vector ALU (DPP and lane swaps; a shuffle goes through LDS and takes ten times
