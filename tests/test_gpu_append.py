@@ -123,6 +123,7 @@ class Setup:
     dict(counts=[1100], lens=[13], Hq=3, Hkv=1, d=80, rot=32, packed=0, block=64), dict(counts=[2, 2], lens=[3, 14], rot=16, Hq=1, Hkv=1),
     dict(counts=[9, 1], lens=[0, 0], bf16=0, d=256, rot=256, Hq=2, Hkv=2), dict(counts=[20, 30], lens=[1, 1], Hq=5, Hkv=5, d=96, rot=48, halves=0),
     dict(counts=[4, 4], lens=[12, 28], packed=0, explicit=1, axes=[10, 11, 11], offset=1),
+    dict(counts=[300, 1, 280], lens=[7, 0, 40], Hq=28, Hkv=4, d=128, rot=128, axes=[16, 24, 24], explicit=1, tail=3), dict(counts=[700], lens=[3], Hq=8, Hkv=2, d=128, rot=128, bf16=0, packed=0),
 ])
 def test_against_definition(kw):
     s = Setup(**kw)
@@ -203,3 +204,17 @@ def test_captured_with_other_lengths_between_replays():
         graph.replay()
         torch.cuda.synchronize()
         s.check()
+
+
+def test_blocks_beyond_32_bits_of_a_pool():
+    """Blocks a gigabyte apart: offsets of the last ones pass 2^32 elements."""
+    s = Setup([20, 3], [10, 0], packed=1)
+    n, gap = s.k.shape[0], (1 << 29) + 1024
+    pools = [torch.empty(gap * (n - 1) + s.k[0].numel(), device="cuda", dtype=torch.bfloat16).as_strided(s.k.shape, (gap,) + s.k.stride()[1:]) for _ in range(2)]
+    assert n >= 9 and gap * (n - 1) > 1 << 32
+    for pool, name in zip(pools, "kv"):
+        pool.copy_(getattr(s, name))
+        setattr(s, name, pool)
+    s.desc.stride_block = gap
+    s.run()
+    s.check()

@@ -125,3 +125,20 @@ def test_other_stream_and_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager * 0.5 ** (k + 1))  # powers of two go through every rounding
+
+
+def test_rows_that_go_past_the_caches_and_beyond_32_bits():
+    """Results of over 4 MB, and rows that lie 2^26 elements apart: the last one begins beyond 2^32 bytes."""
+    rows, H, d = 700, 32, 128
+    x, pos, dev, desc, host, want = _case(rows, H, d, d, 1, 1, [16, 24, 24], 0, 0, 0)
+    out = torch.full((rows + 1, H, d), 7.0, device="cuda", dtype=torch.bfloat16)
+    _run(x, gu.dev(pos), desc, out[:rows], rows, H, d)
+    torch.cuda.synchronize()
+    assert (np.abs(out[:rows].float().cpu().numpy() - want) <= ru.bound(host, want, d, True, True)).all() and (out[rows] == 7.0).all()
+    rows, H, d, apart = 40, 1, 64, 1 << 26
+    x, pos, dev, desc, host, want = _case(rows, H, d, d, 1, 0, [32], 0, 0, 0)
+    far = torch.empty(apart * (rows - 1) + d, device="cuda", dtype=torch.bfloat16).as_strided((rows, H, d), (apart, d, 1))
+    far.copy_(x)
+    _run(far, gu.dev(pos), desc, far, rows, H, d)
+    torch.cuda.synchronize()
+    assert (np.abs(far.float().cpu().numpy() - want) <= ru.bound(host, want, d, False, True)).all()
