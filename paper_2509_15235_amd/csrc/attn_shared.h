@@ -53,13 +53,14 @@ __device__ __forceinline__ char* shared_means(const SharedParams& p, int kvh, in
     return (char*)p.sh_acc + (block * (D / 16) * 64 + half * 32 + (row & 31)) * 16;
 }
 __device__ __forceinline__ char* shared_head(const SharedParams& p, int kvh, int part, int row) { return (char*)p.sh_ml + shared_row(p, kvh, part, row) * 16; }
-// Eight values (both halves' are one piece) as fp16; `exponent`: what gives them back, plus 128. The largest becomes 2^14 .. 2^15.
+// Eight values (both halves' are one piece) as fp16; `exponent`: what gives them back, plus 128. The largest becomes 2^14 .. 2^15, the largest finite
+// one, that is: infinities and NaN of a channel, which stay what they are, cost its neighbours nothing.
 __device__ __forceinline__ u32x4 pack_means(const float (&x)[8], uint32_t& exponent) {
-    float top = fabsf(x[0]);
+    float top = 0.f; // twice the power of two at or below it
 #pragma unroll
-    for (int e = 1; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, __uint_as_float((__float_as_uint(x[e]) + 0x800000u) & 0x7f800000u)); // (the exponent of infinity and NaN wraps to zero)
     top = half_max(top);
-    const int k = min(141 - (int)(__float_as_uint(top) >> 23), 100);
+    const int k = min(142 - (int)(__float_as_uint(top) >> 23), 100);
     exponent = (uint32_t)(128 - k);
     u32x4 w;
 #pragma unroll

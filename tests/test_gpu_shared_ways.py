@@ -157,3 +157,37 @@ def test_large_contiguous_caches_of_one_row_block():
     s.run()
     s.check()
     assert s.k.numel() * 4 > 128e6 and s.k_sh.numel() * 4 > 96e6
+
+
+@pytest.mark.parametrize("way", [1, 2, 3, 4, 5])
+def test_infinite_values_stay_in_their_channel(way, ask):
+    """A shared and an own value that is infinite: that channel of whoever sees it is, and its neighbours are what they are otherwise."""
+    ask(way)
+    s = Shared(12, 4, 8, 2, 128, 500, [40] * 12, q_scale=0.5, mask=1)
+    assert _is(s, way) or way < 3
+    if not _is(s, way):
+        pytest.skip("no way for this call")
+    inf = float("inf")
+    slot = 130  # a shared one; channel 21 of KV head 0
+    s.vs[slot, 0, 21] = inf
+    s.v_sh[int(s.stable_host[slot // 16]), 0, slot % 16, 21] = inf
+    s.vo[3][5, 1, 77] = -inf  # the third sequence's sixth own token
+    s.v[int(s.table_host[3, 0]), 1, 5, 77] = -inf
+    s.run()
+    torch.cuda.synchronize()
+    assert (s.status.cpu() == 0).all()
+    out = s.out.clone()
+    assert (out[:, :, :4, 21] == inf).all() and (out[3, :, 4:, 77] == -inf).all()
+    out[:, :, :4, 21] = 0
+    out[3, :, 4:, 77] = 0
+    assert torch.isfinite(out).all()
+    s.vs[slot, 0, 21] = s.vo[3][5, 1, 77] = 0  # the other channels against the definition
+    s.v_sh[int(s.stable_host[slot // 16]), 0, slot % 16, 21] = 0
+    s.v[int(s.table_host[3, 0]), 1, 5, 77] = 0
+    keep = [(slice(None), slice(None), slice(0, 4), 21), (3, slice(None), slice(4, 8), 77)]
+    s.run()
+    torch.cuda.synchronize()
+    s.check()
+    for at in keep:
+        s.out[at] = 0
+    assert torch.equal(s.out, out)
