@@ -534,7 +534,7 @@ typedef struct vs_append_desc {
  *   prefix_len   [B] int32 in
  *   row_start    [B+1] int32 in, optional, ascending. Where it descends the sequence is reported, and the rows of all are unspecified
  *   q_out        out, the rotated queries, rows of Hq heads; may be q itself with q's stride, and overlaps the inputs in no other way
- *   k_cache, v_cache  out
+ *   k_cache, v_cache  out, two of them; a sequence's slots end where its 32-bit length does
  *   status       [B] int32 out, optional: VS_STATUS_BAD_PREFIX, VS_STATUS_BAD_BLOCK, VS_STATUS_BAD_ROWS
  * Rows of q_out behind the last sequence's and all other slots keep what they hold. Two new tokens never share a slot: no two sequences of a call
  * have the same block where new rows go. prefix_len stays; the caller adds the rows to it, or vs_tree_kv_commit the accepted ones.

@@ -129,7 +129,8 @@ int32_t vs_kv_append(const vs_append_desc* d, const vs_rope_desc* rope, const vo
         if (s > ((int64_t)1 << 40) || (s * eb) % 16) return VS_ERR_LAYOUT;
     for (const void* at : {q, k, v, (const void*)q_out, (const void*)k_cache, (const void*)v_cache})
         if (!aligned16(at) && !(d->Hq == 0 && (at == q || at == q_out))) return VS_ERR_LAYOUT;
-    // two slots in one place: their writes would race
+    // two slots in one place, or a key and a value: their writes would race
+    if (k_cache == v_cache) return VS_ERR_LAYOUT;
     if (!rows_apart(d->d, d->paged ? d->block_size : d->capacity, d->stride_tok, d->Hkv, d->stride_head, d->paged ? d->num_blocks : d->B,
                     d->paged ? d->stride_block : d->stride_seq))
         return VS_ERR_LAYOUT;

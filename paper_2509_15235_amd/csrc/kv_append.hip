@@ -17,7 +17,7 @@ __global__ __launch_bounds__(kRopeThreads) void kv_append_kernel(const AppendPar
     __shared__ int64_t slot_at[kRopeRows]; // bytes from the caches' start to the row's slot of head 0; -1: none
     __shared__ int32_t live[kRopeRows];    // whether the row belongs to a sequence
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int row0 = blockIdx.x * p.rows_per_wg;
+    const int row0 = p.first_row + (int)blockIdx.x * p.rows_per_wg;
     const int rows = min(p.rows_per_wg, (int)(p.rows - row0)), h0 = blockIdx.y * p.heads_per_wg;
     const int all_heads = p.Hq + 2 * p.Hkv;
     const int heads = min(p.heads_per_wg, all_heads - h0), items = rows * p.heads_per_wg * p.rope.chunks;
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kRopeThreads) void kv_append_kernel(const AppendPar
     load(tid);
 
     // ---- wave w: row w's sequence, slot and angles
-    const int64_t have = PAGED ? (int64_t)p.max_blocks << p.block_shift : p.capacity;
+    const int64_t have = min(PAGED ? (int64_t)p.max_blocks << p.block_shift : p.capacity, (int64_t)INT32_MAX); // (a prefix length has 32 bits)
     if (wave < rows) {
         const int row = row0 + wave;
         int seq, i, n = p.T;
@@ -146,12 +146,18 @@ void launch(const AppendParams& p, dim3 grid, hipStream_t s) { p.stream_out ? la
 
 } // namespace
 
-hipError_t launch_kv_append(const AppendParams& p, int dtype, bool halves, hipStream_t s) {
+hipError_t launch_kv_append(AppendParams p, int dtype, bool halves, hipStream_t s) {
     const int all_heads = p.Hq + 2 * p.Hkv;
-    const dim3 grid((unsigned)((p.rows + p.rows_per_wg - 1) / p.rows_per_wg), (unsigned)((all_heads + p.heads_per_wg - 1) / p.heads_per_wg));
-    if (dtype == VS_F32) halves ? launch<true, true>(p, grid, s) : launch<true, false>(p, grid, s);
-    else halves ? launch<false, true>(p, grid, s) : launch<false, false>(p, grid, s);
-    return hipGetLastError();
+    for (int64_t first = 0; first < p.rows; first += kRopeLaunchRows) {
+        const int64_t rows = min(p.rows - first, kRopeLaunchRows);
+        const dim3 grid((unsigned)((rows + p.rows_per_wg - 1) / p.rows_per_wg), (unsigned)((all_heads + p.heads_per_wg - 1) / p.heads_per_wg));
+        p.first_row = (int32_t)first;
+        if (dtype == VS_F32) halves ? launch<true, true>(p, grid, s) : launch<true, false>(p, grid, s);
+        else halves ? launch<false, true>(p, grid, s) : launch<false, false>(p, grid, s);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        p.status = nullptr; // all sequences' are written
+    }
+    return hipSuccess;
 }
 
 } // namespace vs

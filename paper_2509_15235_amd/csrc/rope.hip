@@ -64,11 +64,18 @@ void launch(const RopeApplyParams& p, dim3 grid, hipStream_t s) {
 
 } // namespace
 
-hipError_t launch_rope(const RopeApplyParams& p, int dtype, bool halves, hipStream_t s) {
-    const dim3 grid((unsigned)((p.rows + p.rows_per_wg - 1) / p.rows_per_wg), (unsigned)((p.H + p.heads_per_wg - 1) / p.heads_per_wg));
-    if (dtype == VS_F32) halves ? launch<true, true>(p, grid, s) : launch<true, false>(p, grid, s);
-    else halves ? launch<false, true>(p, grid, s) : launch<false, false>(p, grid, s);
-    return hipGetLastError();
+hipError_t launch_rope(RopeApplyParams p, int dtype, bool halves, hipStream_t s) {
+    for (int64_t left = p.rows; left > 0; left -= kRopeLaunchRows) {
+        p.rows = min(left, kRopeLaunchRows);
+        const dim3 grid((unsigned)((p.rows + p.rows_per_wg - 1) / p.rows_per_wg), (unsigned)((p.H + p.heads_per_wg - 1) / p.heads_per_wg));
+        if (dtype == VS_F32) halves ? launch<true, true>(p, grid, s) : launch<true, false>(p, grid, s);
+        else halves ? launch<false, true>(p, grid, s) : launch<false, false>(p, grid, s);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        p.x = (const char*)p.x + p.rows * p.x_row;
+        p.out = (char*)p.out + p.rows * p.out_row;
+        p.positions += p.rows;
+    }
+    return hipSuccess;
 }
 
 } // namespace vs

@@ -7,6 +7,7 @@ namespace vs {
 
 constexpr int kRopeThreads = 256;                 // four waves, each of which takes a row's angles
 constexpr int kRopeRows = kRopeThreads / kWave;   // rows of a workgroup, at most
+constexpr int64_t kRopeLaunchRows = 1 << 25;       // of a launch: its threads are counted in 32 bits
 constexpr int kRopeBatch = 4;                     // pieces a thread has in flight
 
 // cos and sin of a number of turns in [-1/2, 1/2]. fp32 storage keeps 24 bits of the products, bf16 eight: for those the hardware's

@@ -246,6 +246,7 @@ struct AppendParams {
     int32_t* status;             // may be null
     const int32_t* block_table;  // paged only
     int64_t rows;
+    int32_t first_row;           // of this launch
     int64_t q_row, k_row, v_row, q_out_row; // strides in bytes
     int32_t B, T, Hq, Hkv;
     int32_t row_bytes;           // of a head
@@ -308,7 +309,7 @@ hipError_t launch_accept_sample(SampleParams p, void* workspace, hipStream_t s);
 hipError_t launch_draft_expand(const DraftExpandParams& p, hipStream_t s);
 hipError_t launch_draft_tree_build(const DraftBuildParams& p, hipStream_t s);
 hipError_t launch_kv_commit(const CommitParams& p, hipStream_t s);
-hipError_t launch_rope(const RopeApplyParams& p, int dtype, bool halves, hipStream_t s);
-hipError_t launch_kv_append(const AppendParams& p, int dtype, bool halves, hipStream_t s);
+hipError_t launch_rope(RopeApplyParams p, int dtype, bool halves, hipStream_t s);
+hipError_t launch_kv_append(AppendParams p, int dtype, bool halves, hipStream_t s);
 
 } // namespace vs

@@ -143,3 +143,7 @@ def test_python_calls_pass_their_arguments_on(name):
             getattr(vs, name)(*args, 1)
     finally:
         binding._load_native()
+
+
+def test_one_cache_for_keys_and_values():
+    assert _append(kc=5 * G, vc=5 * G) == -6

@@ -218,3 +218,41 @@ def test_blocks_beyond_32_bits_of_a_pool():
     s.desc.stride_block = gap
     s.run()
     s.check()
+
+
+def test_more_rows_than_one_launch_takes():
+    """2^25 rows and some of one sequence, a key and a value of four channels each; a second sequence behind it."""
+    rows = (1 << 25) + 9
+    k, v = (torch.randn((rows, 4), device="cuda", generator=torch.Generator("cuda").manual_seed(s)) for s in (0, 1))
+    kc, vc = (torch.full((2, rows, 4), 7.0, device="cuda") for _ in range(2))
+    freq, status = gu.dev(ru.frequencies(4)), torch.full((2,), -9, device="cuda", dtype=torch.int32)
+    d = vs.AppendDesc(B=2, T=rows, Hq=0, Hkv=1, d=4, dtype=vs.VS_F32, rows=rows, k_stride=4, v_stride=4, capacity=rows, stride_seq=rows * 4, stride_head=rows * 4, stride_tok=4)
+    rc = vs.vs_kv_append(d, ru.rope_desc(4, False, inv_freq=freq.data_ptr()), None, k, v, None, None, None, gu.dev(np.array([2, 1], dtype=np.int32)),
+                         gu.dev(np.array([0, rows - 4, rows], dtype=np.int32)), None, kc, vc, status, gu.stream_ptr())
+    torch.cuda.synchronize()
+    assert rc == 0 and status.cpu().tolist() == [0, 0]
+    n = rows - 4
+    assert torch.equal(vc[0, 2:2 + n], v[:n]) and torch.equal(vc[1, 1:5], v[n:])
+    assert (vc[0, :2] == 7).all() and (vc[0, n + 2:] == 7).all() and (vc[1, 0] == 7).all() and (vc[1, 5:] == 7).all()
+    at = np.arange(n - 20, n)
+    host = k[n - 20:].cpu().numpy()[:, None]
+    pos = np.concatenate([at + 2, 1 + np.arange(4)])
+    cos, sin = ru.cos_sin(pos[None], ru.frequencies(4), ru.axis_of_pair(2, [2], False))
+    want = ru.rotate(host, cos, sin, 4, False)
+    got = torch.cat([kc[0, n - 18:n + 2], kc[1, 1:5]]).cpu().numpy()[:, None]
+    assert (np.abs(got - want) <= ru.bound(host, want, 4, False, False)).all()
+
+
+def test_slots_end_where_lengths_do():
+    """A cache whose blocks hold more tokens than a length counts: rows that would come behind 2^31 - 1 are refused."""
+    s = Setup([4, 4], [3, 0], block=16, packed=0)
+    s.desc.block_size, s.desc.max_blocks, s.desc.num_blocks = 1 << 30, 4, 2
+    s.table = torch.tensor([[0, 9, 9, 9], [1, 9, 9, 9]], device="cuda", dtype=torch.int32)
+    s.desc.block_table = s.table.data_ptr()
+    s.desc.stride_head, s.desc.stride_tok, s.desc.stride_block = 64 << 30, 64, 128 << 30
+    s.prefix.copy_(torch.tensor([(1 << 31) - 4, (1 << 31) - 3], dtype=torch.int32))
+    s.run()
+    torch.cuda.synchronize()
+    assert s.status.cpu().tolist() == [3, 3]
+    k, v = s.caches()
+    assert (k == 3.0).all() and (v == 5.0).all()

@@ -142,3 +142,18 @@ def test_rows_that_go_past_the_caches_and_beyond_32_bits():
     _run(far, gu.dev(pos), desc, far, rows, H, d)
     torch.cuda.synchronize()
     assert (np.abs(far.float().cpu().numpy() - want) <= ru.bound(host, want, d, False, True)).all()
+
+
+def test_more_rows_than_one_launch_takes():
+    """2^25 rows and some of one head of four channels, on two axes, in place."""
+    rows = (1 << 25) + 7
+    x = torch.randn((rows, 1, 4), device="cuda", generator=torch.Generator("cuda").manual_seed(0))
+    at = torch.cat([torch.arange(5), torch.arange((1 << 25) - 3, rows)])
+    host = x[at.cuda()].cpu().numpy()
+    pos = (torch.arange(2 * rows, device="cuda") % 1009).to(torch.int32).reshape(2, rows)
+    freq = gu.dev(ru.frequencies(4))
+    _run(x, pos, ru.rope_desc(4, False, [1, 1], stride_axis=rows, inv_freq=freq.data_ptr()), x, rows, 1, 4)
+    torch.cuda.synchronize()
+    cos, sin = ru.cos_sin(pos[:, at.cuda()].cpu().numpy(), ru.frequencies(4), ru.axis_of_pair(2, [1, 1], False))
+    want = ru.rotate(host, cos, sin, 4, False)
+    assert (np.abs(x[at.cuda()].cpu().numpy() - want) <= ru.bound(host, want, 4, False, False)).all()
