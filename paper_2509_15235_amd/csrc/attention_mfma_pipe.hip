@@ -891,7 +891,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
             constexpr int G = 2 * DB; // all pieces
 #pragma unroll
             for (int pc = 0; pc < 2 * DB; pc += G) {
-                JoinParts<D == 128 ? 3 : 4, G> parts;
+                JoinParts<D == 128 ? 2 : 3, G> parts;
                 load_parts(row, 0, pc, parts);
                 float x[G][8];
 #pragma unroll

@@ -4,8 +4,8 @@
 // weighted mean o_i of its values; with M the largest reference the row is sum_i 2^(m_i - M) l_i o_i / sum_i 2^(m_i - M) l_i.
 // References and sums are fp32. fp32 storage keeps fp32 means too. For bf16 storage they are what a call writes and reads most of beside K and V (16 x 60
 // nodes of 28 / 4 heads, three parts or so of every row: 47 MB in fp32), so they are kept as fp16 with a power of two of its own for every 16 channels
-// of a row: 11 bits, whatever the values' size, of which 2^29 lie between the largest and the first that loses bits. That rounding, 2^-12, is an eighth of
-// the result's own, 2^-9 at most; a bf16 mean would double what two roundings to bf16 - the weights', the result's - are off by.
+// of a row: 11 bits, whatever the values' size, as long as 2^29 lie between them (else eight, see pack_means). That rounding, 2^-12, is an eighth of the
+// result's own, 2^-9 at most; a bf16 mean would double what two roundings to bf16 - the weights', the result's - are off by.
 #pragma once
 
 #include "attn_mfma_common.h"
@@ -53,13 +53,19 @@ __device__ __forceinline__ char* shared_means(const SharedParams& p, int kvh, in
     return (char*)p.sh_acc + (block * (D / 16) * 64 + half * 32 + (row & 31)) * 16;
 }
 __device__ __forceinline__ char* shared_head(const SharedParams& p, int kvh, int part, int row) { return (char*)p.sh_ml + shared_row(p, kvh, part, row) * 16; }
-// Eight values (both halves' are one piece) as fp16; `exponent`: what gives them back, plus 128. The largest becomes 2^14 .. 2^15, the largest finite
-// one, that is: infinities and NaN of a channel, which stay what they are, cost its neighbours nothing.
+// Eight values (both halves' are one piece) as fp16; `exponent`: what gives them back, plus 128, where the largest becomes 2^14 .. 2^15. The largest finite
+// one, that is: infinities and NaN of a channel, which stay what they are, cost its neighbours nothing. Nor does a channel that is 2^29 times another
+// one, or more: such a piece is kept as bf16, exponent 0, at the price of three bits.
 __device__ __forceinline__ u32x4 pack_means(const float (&x)[8], uint32_t& exponent) {
-    float top = 0.f; // twice the power of two at or below it
+    float top = 0.f, low = -INFINITY; // twice the powers of two at or below the largest and (negative) the smallest, zeros aside
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, __uint_as_float((__float_as_uint(x[e]) + 0x800000u) & 0x7f800000u)); // (the exponent of infinity and NaN wraps to zero)
+    for (int e = 0; e < 8; ++e) {
+        const float power = __uint_as_float((__float_as_uint(x[e]) + 0x800000u) & 0x7f800000u); // (the exponent of infinity and NaN wraps to zero)
+        top = fmaxf(top, power);
+        low = fmaxf(low, __builtin_amdgcn_classf(x[e], 0x267) ? -INFINITY : -power); // (zero, infinity, NaN)
+    }
     top = half_max(top);
+    low = half_max(low);
     const int k = min(142 - (int)(__float_as_uint(top) >> 23), 100);
     exponent = (uint32_t)(128 - k);
     u32x4 w;
@@ -67,6 +73,14 @@ __device__ __forceinline__ u32x4 pack_means(const float (&x)[8], uint32_t& expon
     for (int e = 0; e < 4; ++e) {
         const f32x2 v = {__builtin_amdgcn_ldexpf(x[2 * e], k), __builtin_amdgcn_ldexpf(x[2 * e + 1], k)};
         w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
+    }
+    if (low * -0x1p28f < top) [[unlikely]] { // (the smallest's eleven bits end at fp16's last one)
+        exponent = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const f32x2 v = {x[2 * e], x[2 * e + 1]};
+            w[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+        }
     }
     return w;
 }
@@ -84,6 +98,7 @@ __device__ __forceinline__ SharedRow shared_at(const SharedParams& p, int32_t le
     return {shared_parts(p, len, kvh, row), shared_head(p, kvh, 0, row), shared_means<D>(p, kvh, 0, row, half), (int64_t)p.sh_rows * 16, (int64_t)p.sh_blocks * (kRowBlock * D * 2)};
 }
 constexpr int kJoinHeads = 8; // references in flight
+__device__ __forceinline__ uint32_t piece_exponent(const u32x4& head, int pc) { return ((pc < 4 ? head[2] : head[3]) >> (8 * (pc & 3))) & 0xff; }
 // N parts from s0 on, G pieces from pc on. Past the last part the last one again.
 template <int N, int G>
 struct JoinParts {
@@ -115,9 +130,9 @@ __device__ __forceinline__ float join_reference(const SharedRow& r, const JoinPa
     }
     return m;
 }
-// Adds parts to sums that are relative to the reference M, and to the sum of weights l.
-template <int N, int G>
-__device__ __forceinline__ void join_parts(const SharedRow& r, int s0, int pc, const JoinParts<N, G>& j, float M, float& l, float (&o)[G][8]) {
+// Adds parts to sums that are relative to the reference M, and to the sum of weights l. WIDE: some pieces may be bf16.
+template <bool WIDE, int N, int G>
+__device__ __forceinline__ void add_parts(const SharedRow& r, int s0, int pc, const JoinParts<N, G>& j, float M, float& l, float (&o)[G][8]) {
 #pragma unroll
     for (int s = 0; s < N; ++s) {
         const bool there = s0 + s < r.parts;
@@ -125,17 +140,29 @@ __device__ __forceinline__ void join_parts(const SharedRow& r, int s0, int pc, c
         l += w;
 #pragma unroll
         for (int i = 0; i < G; ++i) {
-            const uint32_t word = pc + i < 4 ? j.head[s][2] : j.head[s][3];
-            const float f = __builtin_amdgcn_ldexpf(w, (int)((word >> (8 * ((pc + i) & 3))) & 0xff) - 128);
+            const uint32_t exponent = piece_exponent(j.head[s], pc + i);
+            const bool wide = WIDE && exponent == 0;
+            const float f = wide ? w : __builtin_amdgcn_ldexpf(w, (int)exponent - 128);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t two = j.x[s][i][e]; // (a cast of the vector's element itself takes the first one)
                 const f16x2 v = __builtin_bit_cast(f16x2, two);
-                o[i][2 * e] = there ? fmaf((float)v[0], f, o[i][2 * e]) : o[i][2 * e];
-                o[i][2 * e + 1] = there ? fmaf((float)v[1], f, o[i][2 * e + 1]) : o[i][2 * e + 1];
+                const float lo = wide ? __uint_as_float(two << 16) : (float)v[0], hi = wide ? __uint_as_float(two & 0xffff0000u) : (float)v[1];
+                o[i][2 * e] = there ? fmaf(lo, f, o[i][2 * e]) : o[i][2 * e];
+                o[i][2 * e + 1] = there ? fmaf(hi, f, o[i][2 * e + 1]) : o[i][2 * e + 1];
             }
         }
     }
+}
+template <int N, int G>
+__device__ __forceinline__ void join_parts(const SharedRow& r, int s0, int pc, const JoinParts<N, G>& j, float M, float& l, float (&o)[G][8]) {
+    bool wide = false;
+#pragma unroll
+    for (int s = 0; s < N; ++s)
+#pragma unroll
+        for (int i = 0; i < G; ++i) wide |= piece_exponent(j.head[s], pc + i) == 0;
+    if (__any(wide)) [[unlikely]] add_parts<true>(r, s0, pc, j, M, l, o);
+    else add_parts<false>(r, s0, pc, j, M, l, o);
 }
 // All of it: j holds the first N parts; on return o, G pieces from pc on, is to be divided by l.
 template <int N, int G>

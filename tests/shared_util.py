@@ -133,17 +133,17 @@ class Shared:
             out[:, h], size[:, h] = w @ vv, w @ np.abs(vv)
         return out, size, most
 
-    def check(self, which=None):
+    def check(self, which=None, wide=0):
         """fp32 arithmetic: a score is off by (d + 4) half units of the sum of its products' sizes, an exponential by 2^-21 beside that, and a sum of n terms
         by n half units; a weight's error counts once above and once below the line. bf16: a weight that meets a value is rounded by half a step, 2^-8, and
-        so is the result."""
+        so is the result; a part's mean once more where some channels dwarf their neighbours (wide)."""
         torch.cuda.synchronize()
         got = self.out.double().cpu().numpy()
         for b in range(self.B) if which is None else which:
             want, size, most = self.want(b)
             n = self.P + int(self.own[b]) + self.T
             off = 2 * ((self.d + 4) * 2.0 ** -24 * most + 2.0 ** -21) + 2 * n * 2.0 ** -24
-            room = off * size + ((size + np.abs(want)) * 2.0 ** -8 if self.bf16 else 2.0 ** -24 * np.abs(want))
+            room = off * size + ((size * (1 + wide) + np.abs(want)) * 2.0 ** -8 if self.bf16 else 2.0 ** -24 * np.abs(want))
             err = np.abs(got[b] - want)
             bad = ~(err <= room)
             assert not bad.any(), (b, int(bad.sum()), float(np.nanmax(err / room)), np.argwhere(bad)[:4].tolist())

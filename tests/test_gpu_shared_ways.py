@@ -191,3 +191,30 @@ def test_infinite_values_stay_in_their_channel(way, ask):
     for at in keep:
         s.out[at] = 0
     assert torch.equal(s.out, out)
+
+
+@pytest.mark.parametrize("exp2", [40, -40, 90, 29, 20])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("way", [1, 2, 3, 4, 5])
+def test_channels_of_very_different_size(way, d, exp2, ask):
+    """Every sixteenth channel of V is a power of two larger (or smaller) than its neighbours; one is zero throughout. All are as accurate as their own size asks."""
+    ask(way)
+    factor = torch.ones(d)
+    factor[5::16] = 2.0 ** exp2
+    factor[9] = 0
+    s = Shared(24, 4, 8, 4, d, 500, [(13 * i) % 70 for i in range(24)], v_scale=factor, q_scale=0.5)
+    if not _is(s, way):
+        pytest.skip("no way for this call")
+    s.run()
+    s.check(wide=exp2 not in (20,))
+    assert (s.out[..., 9] == 0).all()
+
+
+def test_wide_parts_behind_the_pipelined_own_keys():
+    """The same where rows of a sequence's own keys take the pipelined kernel: many sequences of many rows."""
+    for d in (64, 128):
+        factor = torch.ones(d)
+        factor[5::16] = 2.0 ** 40
+        s = Shared(48, 24, 32, 8, d, 300, [(13 * i) % 70 for i in range(48)], v_scale=factor, q_scale=0.5)
+        s.run()
+        s.check(wide=1)
