@@ -248,7 +248,8 @@ size_t vs_shared_prefix_workspace_bytes(const vs_attn_desc* desc, const vs_prefi
  * The descriptor and the arguments describe the sequences' own caches as for vs_tree_verify_attention, with these differences:
  *   - prefix_len[b] (>= 0, at most max_prefix_len) counts the sequence's own tokens only, and its cache holds only those, from logical
  *     slot 0 on, and the tree's nodes behind them. (A paged program with one table row per sequence that names the shared blocks too
- *     passes the address of the rows' first entry of their own, with max_blocks the row length as before; a shared prefix that
+ *     passes the address of the rows' first entry of their own, with max_blocks the row length as before; max_prefix_len + T slots are
+ *     then at most what is left of a row, and no entry behind those is read; a shared prefix that
  *     ends inside a block has its last tokens copied into the sequences' own blocks.) vs_kv_append and vs_tree_kv_commit work on such caches as they are.
  *   - the knobs (impl, num_splits, rows_per_wave, waves_per_group, schedule) have to be 0
  *   k_shared, v_shared  in, layout per prefix (may be the same pools as k_cache and v_cache)

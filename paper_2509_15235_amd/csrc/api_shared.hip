@@ -216,6 +216,7 @@ SharedParams shared_params(const AttnParams& base, const Cut& c, const SharedPla
     p.sh_acc = (float*)workspace;
     p.sh_ml = (float*)((char*)workspace + pl.acc_bytes);
     p.sh_words = (uint64_t*)((char*)p.sh_ml + pl.ml_bytes);
+    if (p.paged) p.capacity = (base.max_prefix_len + base.tree_keys - 1) >> base.block_shift; // see last_entry()
     p.shared_len = shared_len;
     p.shared_table = prefix.paged ? prefix.block_table : nullptr;
     p.sh_batch = d->B;

@@ -53,7 +53,7 @@ __device__ __forceinline__ float row_all(float x, Op op) {
     return op(__uint_as_float(w[0]), __uint_as_float(w[1]));
 }
 
-// MODE: as in attention_mfma_rows.hip. kRowsShared has key splits: of the keys that all sequences share each takes keys_per_split.
+// MODE: as in attn_rows_kernel.h. kRowsShared has key splits: of the keys that all sequences share each takes keys_per_split.
 template <int D, int SETS, bool PAGED, int MODE = kRowsWhole>
 __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const std::conditional_t<MODE == kRowsWhole, AttnParams, SharedParams> p) {
     request_args(p);

@@ -36,7 +36,7 @@ namespace {
 
 // Waves of a SIMD that have registers at the same time: two, and three (workgroups of four waves on a CU) with 64 channels.
 // MODE (attn_shared.h): kRowsShared, all sequences' rows against the keys that they share: equal shares of all row groups' keys, whose pieces
-// leave as partial results in fp32; kRowsOwn, a sequence's rows against its own keys, joined with those.
+// leave as partial results; kRowsOwn, a sequence's rows against its own keys, joined with those.
 template <int D, int RPW, int NW, bool PAGED, bool BAL, bool ONCE, int MODE = kRowsWhole>
 __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma_pipe_kernel(const std::conditional_t<MODE == kRowsWhole, AttnParams, SharedParams> p) {
     request_args(p);
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
     int32_t bt_next = 0;                 // block id of the tile 32 further on
     // (unsigned: rows past the last allowed one may pass 2^31; past the table its last entry is read)
     auto bt_token = [&](int first) __attribute__((always_inline)) { return (uint32_t)k0 + (uint32_t)(first + lane) * kTileKeys + (uint32_t)(block0 * RPI); };
-    auto bt_index = [&](int first) __attribute__((always_inline)) { return min(bt_token(first) >> p.block_shift, (uint32_t)p.max_blocks - 1u); };
+    auto bt_index = [&](int first) __attribute__((always_inline)) { return min(bt_token(first) >> p.block_shift, (uint32_t)last_entry(p)); };
     auto bt_fetch = [&](int first) __attribute__((always_inline)) { return bt_row[bt_index(first)]; };
     auto bt_set = [&](int32_t blk) __attribute__((always_inline)) {
         if ((uint32_t)blk >= (uint32_t)p.num_blocks) blk = 0; // reported through status

@@ -74,7 +74,7 @@
     int32_t bt_win = 0;
     auto bt_fetch = [&]() __attribute__((always_inline)) {
         const int lb = (bt_from + (lane >> 1) * ROUND + (lane & 1) * 16) >> p.block_shift;
-        const int32_t blk = p.block_table[(int64_t)b * p.max_blocks + min(lb, p.max_blocks - 1)];
+        const int32_t blk = p.block_table[(int64_t)b * p.max_blocks + min(lb, last_entry(p))];
         bt_win = (uint32_t)blk < (uint32_t)p.num_blocks ? blk : 0; // a bad entry is reported through status
     };
     if (PAGED) bt_fetch();

@@ -83,8 +83,8 @@ struct AttnParams {
     FastDiv bal_per_seq;        // bal_chunks / B where that is whole; else d = 0
 };
 
-// Attention of a batch behind one shared prefix, in two launches: all sequences' rows against the shared keys, whose partial results stay
-// in fp32, and every sequence's rows against its own keys, joined with them.
+// Attention of a batch behind one shared prefix: all sequences' rows against the shared keys, whose results stay partial ones, and every sequence's rows
+// against its own keys, joined with them; in two launches or in one.
 enum RowsMode { kRowsWhole = 0, kRowsShared = 1, kRowsOwn = 2, kRowsBoth = 3 }; // the kernels of vs_tree_verify_attention; these two; both in one launch
 struct SharedParams : AttnParams {
     float* sh_acc;              // the parts' means (bf16 storage) or sums of weights times values, see attn_shared.h

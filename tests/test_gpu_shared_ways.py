@@ -218,3 +218,26 @@ def test_wide_parts_behind_the_pipelined_own_keys():
         s = Shared(48, 24, 32, 8, d, 300, [(13 * i) % 70 for i in range(48)], v_scale=factor, q_scale=0.5)
         s.run()
         s.check(wide=1)
+
+
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("call", [4, 8, 1, 2])
+def test_rows_of_a_table_that_name_the_shared_blocks_first(call, way, ask):
+    """One table row per sequence, shared blocks and own ones: the own rows begin inside, their distance is the whole row's length, and behind the last one's
+    entries the table ends (nothing there is a block)."""
+    ask(way)
+    kw = dict(CALLS[call], P=640)  # (whole blocks)
+    kw.update(paged=1, max_len=640)
+    s = Shared(**kw)
+    if not _is(s, way):
+        pytest.skip("no way for this call")
+    off, row = len(s.stable_host), s.table_host.shape[1]
+    big = torch.full((s.B * (off + row) + 5000,), 1 << 30, device="cuda", dtype=torch.int32)
+    rows = big[:s.B * (off + row)].view(s.B, off + row)
+    rows[:, :off] = s.stable
+    rows[:, off:] = s.table
+    s.desc.block_table, s.desc.max_blocks = big.data_ptr() + 4 * off, off + row
+    s.pre.block_table = big.data_ptr()
+    assert vs.vs_shared_prefix_workspace_bytes(s.desc, s.pre) == s.ws_bytes
+    s.run()
+    s.check()
