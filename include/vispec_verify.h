@@ -250,7 +250,8 @@ size_t vs_shared_prefix_workspace_bytes(const vs_attn_desc* desc, const vs_prefi
  *     slot 0 on, and the tree's nodes behind them. (A paged program with one table row per sequence that names the shared blocks too
  *     passes the address of the rows' first entry of their own, with max_blocks the row length as before; max_prefix_len + T slots are
  *     then at most what is left of a row, and no entry behind those is read; a shared prefix that
- *     ends inside a block has its last tokens copied into the sequences' own blocks.) vs_kv_append and vs_tree_kv_commit work on such caches as they are.
+ *     ends inside a block has its last tokens copied into the sequences' own blocks.) vs_kv_append and vs_tree_kv_commit work on such caches as they are
+ *     (with rows that begin inside, a length past what is left of a row is not one that they can tell: they take max_blocks entries for theirs).
  *   - the knobs (impl, num_splits, rows_per_wave, waves_per_group, schedule) have to be 0
  *   k_shared, v_shared  in, layout per prefix (may be the same pools as k_cache and v_cache)
  *   shared_len   [1] int32  in, 0 .. max_len; anything else is VS_STATUS_BAD_PREFIX for all sequences, a bad block id
