@@ -257,6 +257,7 @@ size_t vs_shared_prefix_workspace_bytes(const vs_attn_desc* desc, const vs_prefi
  *   shared_len   [1] int32  in, 0 .. max_len; anything else is VS_STATUS_BAD_PREFIX for all sequences, a bad block id
  *                VS_STATUS_BAD_BLOCK for all
  *   workspace    at least vs_shared_prefix_workspace_bytes(desc, prefix) bytes, 256-byte aligned
+ * A node that sees no key at all (a mask word of zero, as vs_tree_mask_build leaves them for an invalid tree, and no tokens in front) gets zeros.
  * The parts of a row's softmax are joined in fp32 before the one rounding to the storage type. B * T * (Hq / Hkv) is at most 1048576, both bounds of
  * lengths at most 2^30.
  */

@@ -334,11 +334,13 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const st
         // two parts per lane of a row: 16 lanes (kb, cg) x 2
         const int q = 2 * (4 * kb + cg);
         const float ma = sm[s][q][j], mb = sm[s][q + 1][j];
-        float M = row_all(fmaxf(ma, mb), [](float x, float y) { return fmaxf(x, y); }); // finite: a node sees itself or the prefix
+        const float top = row_all(fmaxf(ma, mb), [](float x, float y) { return fmaxf(x, y); });
+        // whole attention: finite, a node sees itself or the prefix. Of its own keys a row may see none: weights and sums of zero then
+        const float M = MODE == kRowsWhole ? top : finite_reference(top);
         const float den = row_all(sl[s][q][j] * __builtin_amdgcn_exp2f(ma - M) + sl[s][q + 1][j] * __builtin_amdgcn_exp2f(mb - M),
                                   [](float x, float y) { return x + y; });
         const float f = MODE == kRowsWhole ? __builtin_amdgcn_exp2f(m2[s] - M) / den : __builtin_amdgcn_exp2f(m2[s] - M);
-        if constexpr (MODE != kRowsWhole) row_ml[4 * s + j] = f32x2{M, den}; // (the same from all lanes of a row)
+        if constexpr (MODE != kRowsWhole) row_ml[4 * s + j] = f32x2{top, den}; // (the same from all lanes of a row)
         // registers in the order of their channels: 16 VM of them, halved twice
         float x[16 * VM];
 #pragma unroll
@@ -387,16 +389,17 @@ __global__ __launch_bounds__(kF32Waves * kWave, 2) void attn_f32_kernel(const st
             const int parts = shared_parts(p, p.shared_len[0], kvh, b * p.rows + r);
             float m = row_ml[row][0], l = row_ml[row][1];
             for (int s = 0; s < parts; ++s) {
+                const float before = m;
                 const int64_t from = shared_row(p, kvh, s, b * p.rows + r);
                 const f32x2 ml = *(const f32x2*)(p.sh_ml + from * 2);
-                const float M = fmaxf(m, ml[0]), f = __builtin_amdgcn_exp2f(m - M), g = __builtin_amdgcn_exp2f(ml[0] - M);
+                m = fmaxf(m, ml[0]);
+                const float M = finite_reference(m), f = __builtin_amdgcn_exp2f(before - M), g = __builtin_amdgcn_exp2f(ml[0] - M);
                 l = l * f + ml[1] * g;
-                m = M;
 #pragma unroll
                 for (int e = 0; e < CPT; ++e) o[e] = o[e] * f + p.sh_acc[from * D + c + e] * g;
             }
 #pragma unroll
-            for (int e = 0; e < CPT; ++e) o[e] /= l;
+            for (int e = 0; e < CPT; ++e) o[e] = l == 0.f ? 0.f : o[e] / l;
         }
         float* dst = (float*)p.out + row_start<D>(p, b, kvh) + (uint64_t)row_number(r, row_node(p, r), p.row_skip) * (uint32_t)D + c;
 #pragma unroll

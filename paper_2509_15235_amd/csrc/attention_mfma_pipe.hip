@@ -901,7 +901,7 @@ __global__ __launch_bounds__(NW * 64, D == 64 && NW == 4 ? 3 : 2) void attn_mfma
                 float sum = l;
                 join_row(row, pc, parts, m2[rb], sum, x);
                 if (r_local < p.rows) {
-                    const float inv = 1.f / sum;
+                    const float inv = one_over_sum(sum);
 #pragma unroll
                     for (int i = 0; i < G; ++i)
 #pragma unroll

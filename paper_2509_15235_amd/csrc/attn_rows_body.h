@@ -414,7 +414,7 @@
                 } else {
                     float sum = l;
                     join_row(joined, my_piece, parts, M, sum, r);
-                    inv = 1.f / sum;
+                    inv = one_over_sum(sum);
                 }
             }
 #pragma unroll

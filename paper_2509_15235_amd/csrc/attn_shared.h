@@ -91,6 +91,11 @@ __device__ __forceinline__ u32x4 pack_means(const float (&x)[8], uint32_t& expon
     return w;
 }
 
+// A row that sees no key of a part has the reference -inf there, its weights and sums are zero. Where it sees none at all, this is what they are relative to (else
+// the differences of references would be NaN), and its result is zeros.
+__device__ __forceinline__ float finite_reference(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ float one_over_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
+
 // ---- Joining a row's own part with its parts against the shared keys. Those were written by the launch before, so the first of
 // them are asked for when a workgroup begins, and are there when its own keys are done.
 struct SharedRow { // a lane's row
@@ -170,10 +175,10 @@ __device__ __forceinline__ void join_parts(const SharedRow& r, int s0, int pc, c
     if (__any(wide)) [[unlikely]] add_parts<true>(r, s0, pc, j, M, l, o);
     else add_parts<false>(r, s0, pc, j, M, l, o);
 }
-// All of it: j holds the first N parts; on return o, G pieces from pc on, is to be divided by l.
+// All of it: j holds the first N parts; on return o, G pieces from pc on, is to be divided by l (one_over_sum).
 template <int N, int G>
 __device__ __forceinline__ void join_row(const SharedRow& r, int pc, JoinParts<N, G>& j, float m, float& l, float (&o)[G][8]) {
-    const float M = join_reference(r, j, m), f = __builtin_amdgcn_exp2f(m - M);
+    const float M = finite_reference(join_reference(r, j, m)), f = __builtin_amdgcn_exp2f(m - M);
     l *= f;
 #pragma unroll
     for (int i = 0; i < G; ++i)
