@@ -4,8 +4,8 @@
 // weighted mean o_i of its values; with M the largest reference the row is sum_i 2^(m_i - M) l_i o_i / sum_i 2^(m_i - M) l_i.
 // References and sums are fp32. fp32 storage keeps fp32 means too. For bf16 storage they are what a call writes and reads most of beside K and V (16 x 60
 // nodes of 28 / 4 heads, three parts or so of every row: 47 MB in fp32), so they are kept as fp16 with a power of two of its own for every 16 channels
-// of a row: 11 bits, whatever the values' size, as long as 2^29 lie between them (else eight, see pack_means). That rounding, 2^-12, is an eighth of the
-// result's own, 2^-9 at most; a bf16 mean would double what two roundings to bf16 - the weights', the result's - are off by.
+// of a row: 11 bits for every normal number, as long as 2^29 do not lie between them (else eight, see pack_means). That rounding, 2^-11 at most, is an eighth of the
+// result's own, 2^-8 at most; a bf16 mean would add as much as either of the two roundings to bf16, the weights' and the result's.
 #pragma once
 
 #include "attn_mfma_common.h"
@@ -61,7 +61,8 @@ __device__ __forceinline__ char* shared_means(const SharedParams& p, int kvh, in
 __device__ __forceinline__ char* shared_head(const SharedParams& p, int kvh, int part, int row) { return (char*)p.sh_ml + shared_row(p, kvh, part, row) * 16; }
 // Eight values (both halves' are one piece) as fp16; `exponent`: what gives them back, plus 128, where the largest becomes 2^14 .. 2^15. The largest finite
 // one, that is: infinities and NaN of a channel, which stay what they are, cost its neighbours nothing. Nor does a channel that is 2^29 times another
-// one, or more: such a piece is kept as bf16, exponent 0, at the price of three bits.
+// one, or more: such a piece is kept as bf16, exponent 0, at the price of three bits. The smallest normal number times 2^112 is fp16's smallest: no larger power is
+// needed, and a weight divided by it has bits left (2^-14, the least that can matter beside a weight of one there, becomes 2^-126).
 __device__ __forceinline__ u32x4 pack_means(const float (&x)[8], uint32_t& exponent) {
     float top = 0.f, low = -INFINITY; // twice the powers of two at or below the largest and (negative) the smallest, zeros aside
 #pragma unroll
@@ -72,7 +73,7 @@ __device__ __forceinline__ u32x4 pack_means(const float (&x)[8], uint32_t& expon
     }
     top = half_max(top);
     low = half_max(low);
-    const int k = min(142 - (int)(__float_as_uint(top) >> 23), 100);
+    const int k = min(142 - (int)(__float_as_uint(top) >> 23), 112);
     exponent = (uint32_t)(128 - k);
     u32x4 w;
 #pragma unroll
