@@ -215,9 +215,12 @@ def _load_native():
     _native.bind({name: ctypes.cast(getattr(loaded, name), ctypes.c_void_p).value for name in _NATIVE + _NATIVE_MORE})
 
 
-def _missing(name):
+def _missing(name, why=None):
     def call(*args, **kwargs):
-        raise FileNotFoundError(f"{os.path.join(_HERE, '_native.so')} is missing or out of date: build it with `python -m paper_2509_15235_amd.build`")
+        path, how = os.path.join(_HERE, "_native.so"), "build it with `python -m paper_2509_15235_amd.build`"
+        if why is None:
+            raise FileNotFoundError(f"{path} is missing: {how}")
+        raise ImportError(f"{path} does not fit binding.py ({why}): {how}") from why
     call.__name__ = name
     return call
 
@@ -232,8 +235,8 @@ else:
     try:
         _native.setup(_load_native, _ptr, _scalar, ctypes.byref, ctypes.ArgumentError, AttnDesc, KVDesc, RopeDesc, AppendDesc, PrefixDesc)
         globals().update({name: getattr(_native, name) for name in _NATIVE + _NATIVE_MORE})
-    except (TypeError, AttributeError):  # built from other sources than these: the package can still be imported to build it
-        globals().update({name: _missing(name) for name in _NATIVE + _NATIVE_MORE})
+    except (TypeError, AttributeError) as e:  # built from other sources than these: the package can still be imported to build it
+        globals().update({name: _missing(name, e) for name in _NATIVE + _NATIVE_MORE})
 
 
 def vs_version() -> int:
