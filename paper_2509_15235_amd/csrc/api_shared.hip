@@ -201,6 +201,12 @@ bool reads_once(const vs_attn_desc& d, int tree, const Cut& c, double least) {
            rows_apart(d.d, keys, d.stride_tok, d.Hkv, d.stride_head, d.B, d.stride_seq);
 }
 
+// Which halves of a call do (a bit each, the shared keys' first).
+int32_t once_halves(const vs_attn_desc* d, const vs_attn_desc& prefix, const SharedPlan& pl) {
+    if (pl.way != kWayRows || d->dtype == VS_F32) return 0;
+    return (reads_once(prefix, 0, pl.shared, 96.) ? 1 : 0) | (!pl.own_pipe && reads_once(*d, 1, pl.own, 128.) ? 2 : 0);
+}
+
 SharedParams shared_params(const AttnParams& base, const Cut& c, const SharedPlan& pl, const vs_attn_desc* d, const vs_attn_desc& prefix, const int32_t* shared_len,
                            void* workspace) {
     SharedParams p{};
@@ -255,6 +261,12 @@ int32_t vs_internal_shared_way(const vs_attn_desc* desc, const vs_prefix_desc* p
     return rc != VS_OK ? rc : plan_shared(desc, x).way;
 }
 
+int32_t vs_internal_shared_reads_once(const vs_attn_desc* desc, const vs_prefix_desc* prefix) {
+    vs_attn_desc x;
+    const int32_t rc = check_shared(desc, prefix, x);
+    return rc != VS_OK ? rc : once_halves(desc, x, plan_shared(desc, x));
+}
+
 size_t vs_shared_prefix_workspace_bytes(const vs_attn_desc* desc, const vs_prefix_desc* prefix) {
     vs_attn_desc x;
     if (check_shared(desc, prefix, x) != VS_OK) return 0;
@@ -280,10 +292,9 @@ int32_t vs_shared_prefix_attention(const vs_attn_desc* desc, const vs_prefix_des
                                        shared_len, workspace);
     SharedParams second = shared_params(attention_params(desc, 1, q, k_cache, v_cache, prefix_len, tree_parent, tree_mask, out, status), pl.own, pl, desc, x,
                                         shared_len, workspace);
-    if (pl.way == kWayRows && !f32) {
-        first.once = reads_once(x, 0, pl.shared, 96.);
-        second.once = !pl.own_pipe && reads_once(*desc, 1, pl.own, 128.);
-    }
+    const int32_t once = once_halves(desc, x, pl);
+    first.once = once & 1;
+    second.once = once >> 1;
     hipError_t e;
     if (pl.way == kWayBoth8 || pl.way == kWayBoth4) {
         e = launch_attention_shared_both(first, second, pl.way == kWayBoth8 ? 8 : 4, s);

@@ -279,6 +279,8 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 // the cheapest), and what a call with these descriptors takes (or a vs_error): for tests. A workspace is sized for the way asked for then.
 extern "C" void vs_internal_set_shared_way(int32_t way);
 extern "C" int32_t vs_internal_shared_way(const vs_attn_desc* desc, const vs_prefix_desc* prefix);
+// Which halves of such a call load K and V as data that is read once: 1 the shared keys', 2 the own ones', 3 both (or a vs_error).
+extern "C" int32_t vs_internal_shared_reads_once(const vs_attn_desc* desc, const vs_prefix_desc* prefix);
 
 int32_t check_attention(const vs_attn_desc* d, int tree); // shapes, types and layouts that need no device (api.hip)
 // What a descriptor says, as the kernels take it; the plan's numbers are left at zero (api.hip)
