@@ -57,6 +57,7 @@ enum Way : int32_t {
     kWays = 6
 };
 thread_local int32_t asked_way = kWayAuto; // vs_internal_set_shared_way
+thread_local int32_t asked_own = 0;        // vs_internal_set_shared_own
 struct SharedPlan {
     Cut shared, own;
     int32_t way, own_waves, own_pipe;
@@ -171,6 +172,7 @@ SharedPlan plan_shared(const vs_attn_desc* d, const vs_attn_desc& prefix) {
     //   8 x 10 nodes 15.9 17.0 19.3 / 18.2 22.4 32.2; 16 x 30 21.2 23.0 28.6 / 24.8 29.7 39.0; 16 x 60 33.8 35.9 45.2 / 32.5 36.1 46.5; 32 x 60 53.8 56.4 70.7 / 46.3 50.7 66.4
     // (Two row blocks to a workgroup lose to both: 8 x 10 19.8 20.6 24.2.)
     pl.own_pipe = !f32 && own_rows > 2 * kRowBlock && z.own_units * ((own_rows + kRowBlock - 1) / kRowBlock) > 4 * kNumCUs;
+    if (asked_own && !f32 && !both) pl.own_pipe = asked_own == 2;
     o.rows_per_group = f32 ? (z.own_units * ((own_rows + 3) / 4) <= kNumCUs ? 4 : 8) : pl.own_pipe ? 4 * kRowBlock : kRowBlock;
     o.row_groups = (own_rows + o.rows_per_group - 1) / o.rows_per_group;
     o.num_splits = 1;
@@ -255,6 +257,12 @@ SharedParams shared_params(const AttnParams& base, const Cut& c, const SharedPla
 extern "C" {
 
 void vs_internal_set_shared_way(int32_t way) { asked_way = way; }
+void vs_internal_set_shared_own(int32_t how) { asked_own = how; }
+int32_t vs_internal_shared_own(const vs_attn_desc* desc, const vs_prefix_desc* prefix) {
+    vs_attn_desc x;
+    const int32_t rc = check_shared(desc, prefix, x);
+    return rc != VS_OK ? rc : plan_shared(desc, x).own_pipe ? 2 : 1;
+}
 int32_t vs_internal_shared_way(const vs_attn_desc* desc, const vs_prefix_desc* prefix) {
     vs_attn_desc x;
     const int32_t rc = check_shared(desc, prefix, x);

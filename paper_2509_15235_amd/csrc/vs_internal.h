@@ -279,6 +279,9 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 // the cheapest), and what a call with these descriptors takes (or a vs_error): for tests. A workspace is sized for the way asked for then.
 extern "C" void vs_internal_set_shared_way(int32_t way);
 extern "C" int32_t vs_internal_shared_way(const vs_attn_desc* desc, const vs_prefix_desc* prefix);
+// How the sequences' own keys are worked on in a launch of theirs: 1 a workgroup for every row block, 2 the pipelined kernel (bf16; 0: by the rule); what a call takes.
+extern "C" void vs_internal_set_shared_own(int32_t how);
+extern "C" int32_t vs_internal_shared_own(const vs_attn_desc* desc, const vs_prefix_desc* prefix);
 // Which halves of such a call load K and V as data that is read once: 1 the shared keys', 2 the own ones', 3 both (or a vs_error).
 extern "C" int32_t vs_internal_shared_reads_once(const vs_attn_desc* desc, const vs_prefix_desc* prefix);
 
