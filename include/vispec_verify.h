@@ -231,7 +231,7 @@ int32_t vs_tree_verify_attention(const vs_attn_desc* desc, const void* q, const 
  *   paged      (paged = 1):  blk*stride_block + kv*stride_head + (t % block_size)*stride_tok + c  with  blk = block_table[t / block_size]
  */
 typedef struct vs_prefix_desc {
-    int32_t max_len;        /* host-side upper bound on *shared_len, >= 1; sizes the launch */
+    int32_t max_len;        /* host-side upper bound on *shared_len, >= 1; sizes the launch (a loose one costs time, see below) */
     int32_t paged, block_size, max_blocks, num_blocks; /* as in vs_attn_desc */
     int64_t capacity;       /* contiguous: token slots (for the bounds check) */
     int64_t stride_block;   /* paged */
@@ -253,6 +253,14 @@ size_t vs_shared_prefix_workspace_bytes(const vs_attn_desc* desc, const vs_prefi
  *     ends inside a block has its last tokens copied into the sequences' own blocks.) vs_kv_append and vs_tree_kv_commit work on such caches as they are
  *     (with rows that begin inside, a length past what is left of a row is not one that they can tell: they take max_blocks entries for theirs).
  *   - the knobs (impl, num_splits, rows_per_wave, waves_per_group, schedule) have to be 0
+ * Which of the two calls: with paged caches vs_tree_verify_attention computes the same from tables that name the shared blocks for every sequence. This call is
+ * the faster one where it saves reads that no cache serves: models with a KV head for every query head (32 x 1 token, 32 / 32 heads, 4099 shared tokens: 44 us, the
+ * other call 119), and single tokens or short trees behind several thousand tokens (28 / 4 heads, 64 x 1 behind 8192: 31, 54; 64 x 4 nodes: 53, 58). With grouped heads
+ * behind one or two thousand tokens the other one is as fast or faster (4 x 1 behind 1696: 9.6, 9.3; 64 x 4: 25, 18), and so it is for whole draft trees (16 x 60 nodes
+ * behind 6684: 123, 109), whose products are what bounds both.
+ * The bound max_len: the shared keys are cut into workgroups for a prefix of that length, and those behind *shared_len do nothing. 28 / 4 heads behind 1696 tokens,
+ * max_len 1696 / 4096 / 8192 / 32768: 4 x 1 token 9.8 / 10.3 / 11.2 / 17.1 us, 64 x 4 nodes 25 / 31 / 40 / 54. A program that captures the call keeps a graph for each
+ * of a few bounds.
  *   k_shared, v_shared  in, layout per prefix (may be the same pools as k_cache and v_cache)
  *   shared_len   [1] int32  in, 0 .. max_len; anything else is VS_STATUS_BAD_PREFIX for all sequences, a bad block id
  *                VS_STATUS_BAD_BLOCK for all
@@ -511,7 +519,7 @@ int32_t vs_rope_apply(const vs_rope_desc* rope, const void* x, int64_t x_stride_
  */
 typedef struct vs_append_desc {
     int32_t B;      /* sequences */
-    int32_t T;      /* new rows per sequence; with row_start: the most of any sequence. 1 or more, no upper limit of its own */
+    int32_t T;      /* new rows per sequence; with row_start: the most of any sequence. 1 or more, up to the slots of a sequence's cache */
     int32_t Hq;     /* query heads; 0: keys and values only */
     int32_t Hkv;
     int32_t d;      /* up to 256 */

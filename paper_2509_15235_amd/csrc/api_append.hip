@@ -18,9 +18,12 @@ RowCut cut_rows(int64_t rows, int32_t H, int32_t chunks) {
     return c;
 }
 
-// Whether results go past the L2 caches (nt stores): large ones, which their readers do not find there anyway, and which take the inputs' place there
-// while they are written. us in a graph, plain / past, 32 heads of 128 channels: 500 rows (4.1 MB written) 3.17 / 3.12, 1000 4.42 / 3.84, 2000 7.98 / 6.60,
-// 6684 24.9 / 17.4 (6.3 TB/s), 16000 51.7 / 48.5; appends of 28 / 4 heads, paged: 807 rows (6.8 MB) 5.98 / 5.51, 960 6.34 / 5.65, 7708 34.3 / 24.3 (5.9 TB/s)
+// Whether results go past the L2 caches (nt stores): large ones, which would take the inputs' place there while they are written. us in a graph, three sets of
+// data in turn, plain / past. The call alone, 32 heads of 128 channels: 500 rows (4.1 MB written) 3.12 / 3.13, 600 3.68 / 3.44, 1000 4.34 / 3.81, 2000 8.00 / 6.60,
+// 6684 25.9 / 17.4 (6.3 TB/s), 16000 52.1 / 49.2; appends of 28 / 4 heads, paged: 16 x 60 nodes (8.8 MB) 6.17 / 5.45, 32 x 60 10.2 / 9.0, 7712 rows 34.2 / 24.5 (5.9 TB/s).
+// Who reads the results next pays a part of that back, and from some 30 MB on more, since a plain store would have left him some. The call and a read of all it wrote:
+// 600 rows 8.35 / 7.22, 1000 8.79 / 7.88, 2000 12.7 / 11.8, 4000 18.6 / 19.0, 6684 26.6 / 28.6, 16000 64.8 / 73.3, the append of 7712 rows 39.5 / 35.9; appended trees and
+// the attention behind them: 10 x 60 42.5 / 42.8, 16 x 60 51.5 / 51.3, 32 x 60 70.8 / 70.4, 64 x 60 115.1 / 116.6.
 bool streams_out(int64_t bytes) { return bytes >= (4 << 20); }
 
 int32_t check_rope(const vs_rope_desc* r, int32_t d, int32_t dtype, RopeParams& p) {

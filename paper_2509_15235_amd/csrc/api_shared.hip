@@ -91,12 +91,17 @@ bool cut_rows(const SharedSize& z, int32_t rows_per_group, int64_t places, int32
 int64_t wave_tiles(const Cut& s, int32_t waves) { return (s.keys_per_split / kTileKeys + waves - 1) / waves; }
 
 // One way's plan with its cost, the call's us as a straight line through what was measured; false: not for this call.
-// us per call, 28 / 4 heads of 128 channels and paged caches unless stated, up to 200 own keys, by way Both8 / Both4 / Rows / Line or Units:
-//   4 x 1 token, 1696 keys 10.0 / - / 13.5 / -; 8192 keys 13.5 / - / 20.1 / -; 20 x 1, 600 keys 12.5 / - / - / 21.4, 8192 keys 21.8 / - / - / 25.9
-//   30 x 4, 8192 keys 52 / - / - / 37; 60 x 4, 8 / 1 heads, 8192 keys 23.4 / - / - / 31.9
-//   64 x 1, 600 keys - / 13.8 / 18.0 / 23.2, 1696 keys - / 18.2 / 19.0 / 23.8, 8192 keys - / 31.2 / 30.1 / 33.9; 80 x 1, 8192 keys - / 44.8 / 29.9 / 35.6
-//   64 x 4, 600 keys - / 18.1 / 20.5 / 24.8, 1696 keys - / 26.9 / 24.7 / 27.6, 8192 keys - / 78.6 / 54.8 / 51.7
-//   10 x 1, 32 / 32 heads, 4096 keys - / 20.6 / 24.9 / -; 14 x 1 - / 26.5 / 25.5 / -; 40 x 1, 32 / 8 heads of 64, 8192 keys 15.7 / 21.2 / 19.1 / 27.5
+// us per call in a graph, three sets of data in turn, 28 / 4 heads of 128 channels and paged caches unless stated, 64 .. 200 own keys, by way Both8 / Both4 / Rows / Line /
+// Units, the way that the lines choose in brackets:
+//   4 x 1 token, 1696 keys [9.9] / 10.2 / 13.7 / - / -; 8192 keys [13.7] / 15.7 / 21.0 / - / -; 20 x 1, 600 keys [12.6] / 11.6 / 17.1 / 27.7 / 22.9, 8192 keys [20.3] / 23.2 / 24.5 / 28.0 / 28.0
+//   30 x 4, 8192 keys 53.1 / 39.1 / [33.6] / 34.5 / 34.6; 60 x 4, 8 / 1 heads, 8192 keys [23.9] / 24.0 / 25.5 / 33.8 / 33.7
+//   64 x 1, 600 keys - / [14.1] / 19.3 / 30.0 / 24.9, 1696 keys - / [16.9] / 20.2 / 30.3 / 25.9, 8192 keys - / 29.3 / [31.5] / 35.9 / 35.8; 80 x 1, 8192 keys - / 43.9 / [31.4] / 43.1 / 39.1
+//   64 x 4, 600 keys - / [17.2] / 21.0 / 31.3 / 26.1, 1696 keys - / 26.1 / [25.3] / 34.0 / 28.7, 8192 keys - / 77.3 / 53.8 / 57.6 / [52.4]
+//   16 x 60, 1696 keys - / - / 59.8 / 54.7 / [49.3], 6684 keys, up to 700 own ones - / - / 150.6 / [122.8] / 118.2
+//   10 x 1, 32 / 32 heads, 4096 keys - / [21.2] / 26.4 / - / -; 14 x 1 - / 30.6 / [28.0] / - / -; 40 x 1, 32 / 8 heads of 64, 8192 keys - / 21.8 / [19.4] / 28.6 / 28.5
+// All of them go by the host's bound on the length. Behind 1696 keys with a bound of 1696 / 4096 / 8192 / 32768, by the way chosen then: 4 x 1 9.8 / 10.3 / 11.2 / 17.1;
+// 64 x 4 25.4 / 31.0 / 39.8 / 53.7 (Both4 26.0 throughout, Rows 24.9 / 31.4 / 31.4 / 31.3); 16 x 60 49.7 / - / 64.4 / 64.2. fp32, 6 x 5 nodes of 8 / 2 heads behind 601 keys, bounds of
+// 601 / 4096 / 32768: 15.7 / 19.7 / 19.7.
 bool plan_way(const SharedSize& z, int32_t way, SharedPlan& pl) {
     pl = SharedPlan{};
     pl.way = way;

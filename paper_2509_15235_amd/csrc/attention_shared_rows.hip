@@ -2,7 +2,7 @@
 // sequence's rows against its own, or both in one launch.
 //
 // What bounds them: keys that no other workgroup reads come from memory once, so a batch of decoded tokens is bound by its bytes (32 x 1 token of 32 / 32 heads behind 4099
-// keys, up to 300 own ones: 67 MB of shared keys in 13.8 us, 4.9 TB/s, the own ones' 87 in 26, workgroups that begin and end); a few rows by the
+// keys, up to 300 own ones: 67 MB of shared keys in 13.7 us, 4.9 TB/s, the own ones' 87 in 27, workgroups that begin and end); a few rows by the
 // trips in a row - length, tiles, merge of the waves, arrival, join - 10.3 us for 4 x 1 token of 28 / 4 heads behind 1696 keys, one launch. From some 200 rows of a KV head
 // on the matrix instructions bound the call, and the pipelined kernel takes the shared keys (attention_mfma_pipe.hip); which way a call goes is api_shared.hip's.
 #include "attn_rows_kernel.h"

@@ -5,7 +5,7 @@
 // prefix length, its block id. A workgroup takes up to four consecutive rows, whatever sequences they belong to - so packed sequences
 // of very different lengths leave no workgroup idle - and some of their heads; wave w finds row w's sequence (the row_start entries that do not
 // lie behind it are counted 64 at a time), works out its slot and its angles, while all threads' first pieces are on their way.
-// Measured, 28 / 4 heads of 128 bf16 channels: twelve packed prompts of 7708 rows in all 23.9 us (5.9 TB/s); 16 trees of 60 nodes, paged, 6.2 us; one token 3.6 us.
+// Measured, 28 / 4 heads of 128 bf16 channels: twelve packed prompts of 7712 rows in all 24.0 us (5.9 TB/s); 16 trees of 60 nodes, paged, 6.0 us; one token 3.5 us.
 #include "rope_device.h"
 
 namespace vs {

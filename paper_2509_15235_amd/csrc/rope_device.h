@@ -64,7 +64,7 @@ __device__ __forceinline__ uint32_t to_bf16x2(float lo, float hi) {
     const f32x2 v = {lo, hi};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
 }
-// STREAM: what is written will not be read out of a cache that it would have to itself, see streams_out().
+// STREAM: past the L2 caches, see streams_out().
 template <bool STREAM>
 __device__ __forceinline__ void put(char* to, u32x4 w) {
     if constexpr (STREAM) __builtin_nontemporal_store(w, (u32x4*)to);
